@@ -23,7 +23,7 @@
  *     overrides of lisa_tune_set(), none of which a call needs.
  *   - Return value: 0 (LISA_OK) or a negative lisa_status.  All argument validation is
  *     done on the host before any HIP call, so a rejected call has touched nothing.
- *   - Tensors are dense, row-major, innermost index last, base pointers 16-byte aligned.
+ *   - Tensors are dense, row-major, innermost index last, base pointers 16-byte aligned (int32 arrays: 4-byte).
  *   - Element types: `dtype` is the type of Q, K, V, Q_LR, K_LR, W1, W2 and of the
  *     attention output O (float32 instead when out_f32 = 1: the accumulators are float32
  *     and rounding O to bfloat16 alone costs up to 2^-9 of each element).  Score tensors
@@ -83,7 +83,7 @@ typedef enum {
 
 typedef enum {
   LISA_WS_PREFILL = 0, LISA_WS_DECODE = 1, LISA_WS_STD = 2, LISA_WS_LAYER = 3, LISA_WS_LAYER_DECODE = 4,
-  LISA_WS_KD = 5
+  LISA_WS_KD = 5, LISA_WS_DECODE8 = 6, LISA_WS_STD_DECODE8 = 7
 } lisa_ws_kind;
 
 /* Problem descriptor (host memory, plain data, zero-initialise then fill). */
@@ -386,6 +386,114 @@ int lisa_kd_huber(const lisa_desc* desc, const void* scores, const void* teacher
                   float weight, int accumulate, double* out, void* workspace,
                   size_t workspace_bytes, void* hip_stream);
 
+/*
+ * The paged 8-bit cache: K_LR (or K) and V of the decoding stage (Sec. 5.2) in 8 bits, for sequences of different
+ * lengths that come and go.  A page holds LISA_PAGE_TOKENS tokens of one layer; per page and key/value head
+ *   k   [ceil(width / 8), 64, 8]   codes of the key rows (width = r: K_LR, d_k: K of a standard layer, 0: none, a
+ *                                  direct-sharing layer keeps V alone); element (p, t, e) is feature 8 p + e of token t,
+ *                                  features past the width are zeros
+ *   v   [d_k, 64]                  codes of the value rows
+ *   k_scale, v_scale               float32, a power of two: code c stands for c * scale
+ * Codes are whole numbers -127 .. 127 (LISA_CACHE_INT8; NaN is stored as 0) or OCP e4m3 numbers (LISA_CACHE_E4M3); rounding is to
+ * nearest even, infinities become the largest code.  The scale of a block (page, head) is 2^e with the smallest e >= -126
+ * for which its largest finite magnitude is at most 127 (448) * 2^e.  It grows when a token is appended that needs it, and the
+ * block's codes are then rounded again: the value that a code stands for is within one step (e4m3: of its binade) of what
+ * was appended however often that happens.  Appending token by token and all at once can differ by that much.
+ * One page table serves the pools of all layers.
+ */
+#define LISA_PAGE_TOKENS 64
+typedef enum { LISA_CACHE_INT8 = 0, LISA_CACHE_E4M3 = 1 } lisa_cache_format;
+typedef struct lisa_cache8 {
+  int32_t format;           /* lisa_cache_format                                               */
+  int32_t n_pages;          /* pages of the pool                                               */
+  int32_t max_pages;        /* columns of the page table                                       */
+  int32_t Hkv;              /* key/value heads                                                 */
+  int32_t width;            /* features of a key row (0: no keys)                              */
+  int32_t d_k;              /* features of a value row                                         */
+  void* k;                  /* [n_pages, Hkv, ceil(width / 8), 64, 8]   (NULL: width 0)        */
+  float* k_scale;           /* [n_pages, Hkv]                           (NULL: width 0)        */
+  void* v;                  /* [n_pages, Hkv, d_k, 64]                                         */
+  float* v_scale;           /* [n_pages, Hkv]                                                  */
+  const int32_t* table;     /* [B, max_pages] page of tokens 64 c .. 64 c + 63 of a sequence.  An entry that is no
+                               page of the pool (-1) stands for tokens that nobody sees: nothing is
+                               stored for them, they are not attended, their scores are not written. */
+  const int32_t* lens;      /* [B] tokens of a sequence, the new one among them.  Those past max_pages * 64 (and, in a
+                               decode step, past the descriptor's Lk) do not count; a sequence may have none. */
+} lisa_cache8;
+
+/*
+ * lisa_cache8_append -- stores the last counts[b] of the lens[b] tokens of every sequence: a prompt's, or the new one
+ * of a decode step.  Uses dtype, B, Lq (rows of k_new and v_new), Hkv, r (= width) and d_k of the descriptor.
+ *   k_new [B,Hkv,Lq,width]   in   row i: token lens[b] - counts[b] + i (NULL: width 0)
+ *   v_new [B,Hkv,Lq,d_k]     in
+ *   counts [B]               in   int32, taken to lie in 0 .. min(Lq, lens[b]); NULL: Lq
+ * Writes the codes of these tokens, the scales of the blocks they lie in and, where a scale grows, the codes of the tokens in
+ * front of them in the page; what lies behind a sequence's end in its last page stays as it is.  A page that a new token lies in
+ * must belong to one sequence (lisa_pages_fork sees to that).  The call may be repeated.  No workspace.
+ */
+int lisa_cache8_append(const lisa_desc* desc, const lisa_cache8* cache, const void* k_new, const void* v_new,
+                       const int32_t* counts, void* hip_stream);
+
+/*
+ * lisa_attn_decode8 / std_attn_decode8 -- the decode step of lisa_attn_decode and of std_attn_scores (Lq = 1) against an
+ * 8-bit cache that holds the new token already.  desc: dtype, B, H, Hkv, d_k, r, F, mix, act, scales, write_scores, out_f32 as there,
+ * Lq = 1, Lk = width of the score rows and an upper bound of the lengths (<= max_pages * 64); causal, Lmax and kcache_dim_major are not
+ * used.  Sequence b attends its first min(lens[b], Lk) tokens; the score rows' entries past them are neither read nor written, a
+ * sequence without tokens gives zeros.
+ *   q_lr [B,H,r] / q [B,H,d_k]   in   (q_lr NULL: LISA_MIX_SHARE)
+ *   score_row_prev [B,H,Lk]      in   A_{n-1}, score type
+ *   w1, w2                       in   as in lisa_attn_decode
+ *   out [B,H,d_k]                out
+ *   score_row_out [B,H,Lk]       out  (std_attn_decode8: NULL where it is not wanted)
+ *   workspace   at least lisa_workspace_bytes(desc, LISA_WS_DECODE8 / LISA_WS_STD_DECODE8) bytes
+ */
+int lisa_attn_decode8(const lisa_desc* desc, const lisa_cache8* cache, const void* q_lr, const void* score_row_prev,
+                      const void* w1, const void* w2, void* out, void* score_row_out, void* workspace,
+                      size_t workspace_bytes, void* hip_stream);
+int std_attn_decode8(const lisa_desc* desc, const lisa_cache8* cache, const void* q, void* score_row_out, void* out,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The pages of a server's sequences.  All state is on the device and every call is enqueued like any other, so a step needs no
+ * answer from the device; what a call could not do it says in `done`.  Results depend on the state and the arguments alone: sequences and
+ * requests are served in the order of their index, free pages are given in ascending order.
+ */
+typedef struct lisa_pages {
+  int32_t n_pages;          /* pages of every pool, below 2^20                                 */
+  int32_t n_seqs;           /* rows of the table                                               */
+  int32_t max_pages;        /* columns of the table                                            */
+  int32_t reserved;         /* 0                                                               */
+  int32_t* table;           /* [n_seqs, max_pages]   -1 where there is no page                 */
+  int32_t* lens;            /* [n_seqs] tokens                                                 */
+  int32_t* refs;            /* [n_pages] how often the table names the page; 0: free           */
+} lisa_pages;
+/* Scratch bytes of the lisa_pages_* calls on this state (0: not a valid one). */
+size_t lisa_pages_workspace_bytes(const lisa_pages* pages);
+/* Sequence s gets add[s] >= 0 more tokens and the pages they need: lens, table and refs.  done[s] [n_seqs] = 1, or 0 and the
+ * sequence is as it was: add[s] < 0, more tokens than its row has room for, or not enough free pages (then no sequence behind
+ * it gets pages either). */
+int lisa_pages_grow(const lisa_pages* pages, const int32_t* add, int32_t* done, void* workspace,
+                    size_t workspace_bytes, void* hip_stream);
+/* Sequence dst[i], which must be empty, becomes what src[i] is.  Full pages are shared; a last page that is not full is to be
+ * copied before it is written to: copies[i] = (page, its copy), (-1, -1) where there is none (lisa_pages_copy, for every layer).
+ * n <= n_seqs.  done[i] [n] = 1, or 0 and nothing changed: an index out of range, src[i] = dst[i], dst[i] not empty or named
+ * by a request in front, no free page (then no request behind it gets one either).  Lengths are those before the call. */
+int lisa_pages_fork(const lisa_pages* pages, const int32_t* src, const int32_t* dst, int32_t n, int32_t* done,
+                    int32_t* copies, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* The sequences seqs[i] give their pages back and are empty; done[i] [n] = 0 where the index is out of range or named
+ * in front.  n <= n_seqs. */
+int lisa_pages_free(const lisa_pages* pages, const int32_t* seqs, int32_t n, int32_t* done, void* workspace,
+                    size_t workspace_bytes, void* hip_stream);
+/* The n used pages take the places 0 .. n - 1: used pages behind them go, in ascending order, to the free places in front, in
+ * ascending order.  copies [n_pages / 2, 2] = (from, to), then (-1, -1); lisa_pages_copy has to follow for every layer. */
+int lisa_pages_compact(const lisa_pages* pages, int32_t* copies, void* workspace, size_t workspace_bytes,
+                       void* hip_stream);
+/* Copies pages copies[i][0] of every cache (codes and scales) to pages copies[i][1], all of them as they were before the call as
+ * long as no page is named twice as a target nor both as source and as target; pairs with a number that is no page are passed over.
+ * caches: HOST array, all with the same n_pages. */
+int lisa_pages_copy(const lisa_cache8* caches, int32_t n_caches, const int32_t* copies, int32_t n_copies,
+                    void* hip_stream);
+
 /* Scratch bytes the given entry point (lisa_ws_kind) needs for this descriptor. */
 size_t lisa_workspace_bytes(const lisa_desc* desc, int which);
 /* Bytes of one score tensor of the descriptor in the score type and in its layout (Sec. 5.2:
@@ -404,7 +512,7 @@ const char* lisa_strerror(int status);
 const char* lisa_last_hip_error(void);
 /* Name of the kernel family the last successful call on this thread dispatched to
  * ("generic", "mfma_fused", "mfma_std", "decode_split", "cache_fill", "project_generic",
- * "project_mfma", "project_skinny", "mfma_scores"); for tests and
+ * "project_mfma", "project_skinny", "mfma_scores", "cache8_append", "decode8_generic", "decode8", "pages"); for tests and
  * benchmark reports. */
 const char* lisa_last_path(void);
 

@@ -27,6 +27,12 @@ inline bool score_rows_aligned(const lisa_desc* d) { return d->score_tiled ? d->
 
 int hip_fail(hipError_t e);          // remembers the error's text for lisa_last_hip_error()
 int check_launch();
+// lisa_api.hip: the checks of a descriptor, the path that lisa_last_path() tells
+int check_common_desc(const lisa_desc* d);
+int check_lisa_desc(const lisa_desc* d);
+void note_path(const char* name);
+// cache8_api.hip
+size_t decode8_bytes(const lisa_desc* d, bool lisa_layer);
 
 // ---- optional stage timing (lisa_profile_*) -------------------------------------------
 struct ProfRec {

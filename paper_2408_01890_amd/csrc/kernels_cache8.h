@@ -1,0 +1,259 @@
+// The paged 8-bit cache (Sec. 5.2: what the decoding stage keeps of K_LR, or K, and V): appending tokens to it, and the
+// shape-generic kernels of a decode step over it.
+//
+// A page holds 64 tokens of a layer. Per page and key/value head:
+//   K  [ceil(w / 8)][64][8]  codes of the key rows, features in pieces of 8 (the last one filled up with zeros): 8 bytes of a
+//                            token are what a lane of the 16x16x32 8-bit MFMAs holds of an operand row
+//   V  [d_k][64]             codes of the value rows, tokens innermost: the keys are what P V sums over
+//   one scale each, a power of two: code c stands for c * scale.
+// The scale of a block is 2^e with the smallest e >= -126 for which the block's largest finite |x| is at most top * 2^e (top =
+// 127: whole numbers, 448: e4m3).  When a token arrives that does not fit, the scale grows and the block's codes are rounded
+// again.  Powers of two keep that harmless: a code loses bits by halves, so the error stays within one step of the
+// final scale however often it grows, and every product with a scale is exact.  (With s = max / 127 a code of 10 is
+// rounded back to 10 at each growth by 4 %, and stands for twice the value after 18 of them.)
+#pragma once
+#include "kernels_generic.h"
+
+namespace lisa {
+
+constexpr int PG_TOK = 64;       // LISA_PAGE_TOKENS
+
+// ---- codes ------------------------------------------------------------------------------------
+// FMT: lisa_cache_format.
+template <int FMT> struct code8;
+template <> struct code8<0> {                                // whole numbers
+  static constexpr unsigned TOP_MANTISSA = 0x7e0000u;        // 127 = 1.984375 * 2^6
+  static constexpr int TOP_EXP = 6;
+  static __device__ __forceinline__ float load(unsigned char c) { return (float)(signed char)c; }
+  static __device__ __forceinline__ unsigned char store(float x) {   // NaN has no code: 0
+    const float y = rintf(__builtin_amdgcn_fmed3f(x, -127.f, 127.f));
+    return (unsigned char)(x == x ? (int)y : 0);
+  }
+};
+template <> struct code8<1> {                                // e4m3
+  static constexpr unsigned TOP_MANTISSA = 0x600000u;        // 448 = 1.75 * 2^8
+  static constexpr int TOP_EXP = 8;
+  static __device__ __forceinline__ float load(unsigned char c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
+  static __device__ __forceinline__ unsigned char store(float x) {
+    const float y = __builtin_amdgcn_fmed3f(x, -448.f, 448.f);
+    return x == x ? (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 0xff) : (unsigned char)0x7f;
+  }
+};
+
+// The scale of a block whose largest finite magnitude is m.
+template <int FMT>
+__device__ __forceinline__ float block_scale(float m) {
+  const unsigned u = __float_as_uint(m);
+  int e = (int)(u >> 23) - 127 - code8<FMT>::TOP_EXP + ((u & 0x7fffffu) > code8<FMT>::TOP_MANTISSA ? 1 : 0);
+  e = max(e, -126);                                          // (0 and subnormal numbers among them)
+  return __uint_as_float((unsigned)(e + 127) << 23);
+}
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a < INFINITY ? a : 0.f;
+}
+
+struct Cache8View {
+  unsigned char* k;
+  float* k_scale;
+  unsigned char* v;
+  float* v_scale;
+  const int* table;      // [B][max_pages]
+  const int* lens;       // [B]
+  int n_pages, max_pages, Hkv, w, w8, dk;   // w8: w rounded up to 8
+  __device__ __forceinline__ unsigned char* k_block(int page, int kv) const { return k + ((size_t)page * Hkv + kv) * (w8 * PG_TOK); }
+  __device__ __forceinline__ unsigned char* v_block(int page, int kv) const { return v + ((size_t)page * Hkv + kv) * (dk * PG_TOK); }
+  // The page of column `col` of sequence b; negative where there is none.
+  __device__ __forceinline__ int page_of(int b, int col) const {
+    if ((unsigned)col >= (unsigned)max_pages) return -1;
+    const int p = table[(size_t)b * max_pages + col];
+    return (unsigned)p < (unsigned)n_pages ? p : -1;
+  }
+};
+
+// ---- append -----------------------------------------------------------------------------------
+// The last counts[b] tokens of sequence b (all L rows where counts is null) go into its pages.
+// grid (pages that L tokens can touch, Hkv, B), block 256: a workgroup has one page of one head: the largest
+// magnitudes of its new keys and values, the scales, then the codes; values are turned through the LDS into rows of tokens.
+constexpr int C8_VROW = PG_TOK + 4;      // bytes of a feature's row of codes in the LDS
+template <typename T, int FMT>
+__global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __restrict__ k_new, const T* __restrict__ v_new,
+                                                       const int* __restrict__ counts, int L) {
+  __shared__ __align__(16) unsigned char v_s[256 * C8_VROW];
+  __shared__ float m_s[2][4];
+  const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int len = c.lens[b], n_new = min(max(counts ? counts[b] : L, 0), min(L, len));
+  if (n_new <= 0) return;
+  const int col = (len - n_new) / PG_TOK + (int)blockIdx.x;
+  if ((long long)col * PG_TOK >= len) return;
+  const int page = c.page_of(b, col);
+  if (page < 0) return;
+  const int lo = max(len - n_new - col * PG_TOK, 0), hi = min(len - col * PG_TOK, PG_TOK);
+  const size_t row0 = ((size_t)b * c.Hkv + kv) * L + (col * PG_TOK + lo - (len - n_new));
+  const T* ks = k_new + row0 * c.w;
+  const T* vs = v_new + row0 * c.dk;
+  const int n = hi - lo;
+  float mk = 0.f, mv = 0.f;
+  for (int e = tid; e < n * c.w; e += 256) mk = fmaxf(mk, finite_abs(elem<T>::load(ks + e)));
+  for (int e = tid; e < n * c.dk; e += 256) mv = fmaxf(mv, finite_abs(elem<T>::load(vs + e)));
+  mk = wave_max(mk), mv = wave_max(mv);
+  if ((tid & 63) == 0) m_s[0][tid >> 6] = mk, m_s[1][tid >> 6] = mv;
+  const size_t at = (size_t)page * c.Hkv + kv;
+  const float k_old = c.w ? c.k_scale[at] : 0.f, v_old = c.v_scale[at];
+  __syncthreads();
+  mk = fmaxf(fmaxf(m_s[0][0], m_s[0][1]), fmaxf(m_s[0][2], m_s[0][3]));
+  mv = fmaxf(fmaxf(m_s[1][0], m_s[1][1]), fmaxf(m_s[1][2], m_s[1][3]));
+  float k_now = block_scale<FMT>(mk), v_now = block_scale<FMT>(mv);
+  if (lo) k_now = fmaxf(k_now, k_old), v_now = fmaxf(v_now, v_old);   // (tokens that are there already count too)
+  if (tid == 0) {
+    if (c.w) c.k_scale[at] = k_now;
+    c.v_scale[at] = v_now;
+  }
+  typedef code8<FMT> Code;
+  // keys: 8 features of a token at a time
+  unsigned char* kb = c.k_block(page, kv);
+  const float k_inv = 1.f / k_now;
+  for (int e = tid; e < n * (c.w8 / 8); e += 256) {
+    const int t = e % n, p = e / n;
+    unsigned long long x = 0;
+    for (int f = 0; f < 8; ++f)
+      if (8 * p + f < c.w)
+        x |= (unsigned long long)Code::store(elem<T>::load(ks + (size_t)t * c.w + 8 * p + f) * k_inv) << (8 * f);
+    *(unsigned long long*)(kb + ((size_t)p * PG_TOK + lo + t) * 8) = x;
+  }
+  if (lo && k_now > k_old)
+    for (int e = tid; e < lo * (c.w8 / 8); e += 256) {
+      unsigned long long* at8 = (unsigned long long*)(kb + ((size_t)(e / lo) * PG_TOK + e % lo) * 8);
+      const unsigned long long x = *at8;
+      unsigned long long y = 0;
+      for (int f = 0; f < 8; ++f)
+        y |= (unsigned long long)Code::store(Code::load((unsigned char)(x >> (8 * f))) * k_old * k_inv) << (8 * f);
+      *at8 = y;
+    }
+  // values: through the LDS, [feature][token]
+  unsigned char* vb = c.v_block(page, kv);
+  const float v_inv = 1.f / v_now;
+  const int from = lo && v_now > v_old ? 0 : lo;              // tokens to write
+  for (int e = tid; e < n * c.dk; e += 256) v_s[(e % c.dk) * C8_VROW + lo + e / c.dk] = Code::store(elem<T>::load(vs + e) * v_inv);
+  for (int e = tid; e < (lo - from) * c.dk; e += 256) {
+    const int f = e / lo, t = e % lo;
+    v_s[f * C8_VROW + t] = Code::store(Code::load(vb[f * PG_TOK + t]) * v_old * v_inv);
+  }
+  __syncthreads();
+  for (int e = tid; e < c.dk * 16; e += 256) {               // 4 tokens of a feature at a time
+    const int f = e >> 4, t = 4 * (e & 15);
+    const unsigned x = *(const unsigned*)(v_s + f * C8_VROW + t);
+    unsigned char* dst = vb + f * PG_TOK + t;
+    if (t >= from && t + 4 <= hi) {
+      *(unsigned*)dst = x;
+    } else {
+      for (int u = 0; u < 4; ++u)
+        if (t + u >= from && t + u < hi) dst[u] = (unsigned char)(x >> (8 * u));
+    }
+  }
+}
+
+// ---- decode step, any shape ---------------------------------------------------------------------
+// Scores of one page (64 keys) of one sequence, all heads; float32 arithmetic.  The stages of k_lisa_scores; `mix` 4: the
+// standard layer's q K^T.  exact [B][H][Lk] float32, -inf at keys that have no page; `scores` may be null.
+// grid (ceil(Lk / 64), B), block 256.
+template <typename T, typename S, int FMT>
+__global__ __launch_bounds__(256) void k_cache8_scores(Cache8View c, const T* __restrict__ q, const S* __restrict__ prev,
+                                                       const T* __restrict__ w1, const T* __restrict__ w2, S* __restrict__ scores,
+                                                       float* __restrict__ exact, int H, int Lk, int F, int mix, int act, float scale) {
+  extern __shared__ float c8_sm[];
+  const bool concat = mix == 1, has_ffn = mix <= 1, has_delta = mix != 3, has_prev = mix != 4;
+  const int Din = concat ? 2 * H : H;
+  float* xs = c8_sm;
+  float* hs = xs + Din * 64;
+  float* ds = hs + F * 64;
+  const int col = blockIdx.x, b = blockIdx.y;
+  const int len = min(c.lens[b], Lk);
+  const int pj = threadIdx.x & 63, sl = threadIdx.x >> 6;
+  const int j = col * PG_TOK + pj;
+  if (col * PG_TOK >= len) return;
+  const int page = c.page_of(b, col);
+  const bool live = j < len && page >= 0;
+  const int group = H / c.Hkv;
+  const size_t row = (size_t)b * H * Lk + j;                 // + h * Lk
+  for (int h = sl; h < H; h += 4) {
+    float acc = 0.f, x = 0.f;
+    if (live) {
+      if (has_delta) {
+        const T* qp = q + ((size_t)b * H + h) * c.w;
+        const unsigned char* kp = c.k_block(page, h / group) + pj * 8;
+        for (int t = 0; t < c.w; ++t) acc += elem<T>::load(qp + t) * code8<FMT>::load(kp[(t >> 3) * (PG_TOK * 8) + (t & 7)]);
+        acc *= c.k_scale[(size_t)page * c.Hkv + h / group] * scale;
+      }
+      if (has_prev) x = elem<S>::load(prev + row + (size_t)h * Lk);
+    }
+    if (!has_ffn) {
+      if (live && scores) elem<S>::store(scores + row + (size_t)h * Lk, x + acc);
+      if (j < len) exact[row + (size_t)h * Lk] = live ? x + acc : -INFINITY;
+      continue;
+    }
+    ds[h * 64 + pj] = acc;
+    xs[h * 64 + pj] = x;
+    if (concat) xs[(H + h) * 64 + pj] = acc;
+  }
+  if (!has_ffn) return;
+  __syncthreads();
+  for (int f = sl; f < F; f += 4) {
+    float acc = 0.f;
+    for (int ch = 0; ch < Din; ++ch) acc += xs[ch * 64 + pj] * elem<T>::load(w1 + (size_t)ch * F + f);
+    hs[f * 64 + pj] = act == 0 ? fmaxf(acc, 0.f) : act == 1 ? acc / (1.f + expf(-acc)) : acc;
+  }
+  __syncthreads();
+  for (int h = sl; h < H; h += 4) {
+    float acc = 0.f;
+    if (act == 2) {
+      acc = hs[h * 64 + pj];
+    } else {
+      for (int f = 0; f < F; ++f) acc += hs[f * 64 + pj] * elem<T>::load(w2 + (size_t)f * H + h);
+    }
+    if (!concat) acc += ds[h * 64 + pj];
+    if (live && scores) elem<S>::store(scores + row + (size_t)h * Lk, acc);
+    if (j < len) exact[row + (size_t)h * Lk] = live ? acc : -INFINITY;
+  }
+}
+
+// Softmax over the tokens of a sequence and P V, one head of one sequence per workgroup; float32 arithmetic, zeros where no
+// key is seen.  grid (H, B), block 256 (d_k <= 256).
+template <typename T, typename O, int FMT>
+__global__ __launch_bounds__(256) void k_cache8_softmax_v(Cache8View c, const float* __restrict__ exact, O* __restrict__ out, int H, int Lk) {
+  __shared__ float p_s[PG_TOK], alpha_s;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int kv = h / (H / c.Hkv), len = min(c.lens[b], min(Lk, c.max_pages * PG_TOK));
+  const float* a = exact + ((size_t)b * H + h) * Lk;
+  float m_run = -INFINITY, l_run = 0.f, acc = 0.f;           // (m_run, l_run: the first wave)
+  for (int col = 0; col * PG_TOK < len; ++col) {
+    const int page = c.page_of(b, col);
+    if (page < 0) continue;                                  // (uniform)
+    if (tid < 64) {
+      const int j = col * PG_TOK + tid;
+      const float s = j < len ? a[j] : -INFINITY;
+      const float m_new = fmaxf(m_run, wave_max(s));
+      const float m0 = m_new == -INFINITY ? 0.f : m_new;
+      const float p = j < len ? __expf(s - m0) : 0.f;
+      const float alpha = __expf(m_run - m0);
+      l_run = l_run * alpha + wave_sum(p);
+      m_run = m_new;
+      p_s[tid] = p;
+      if (tid == 0) alpha_s = alpha;
+    }
+    __syncthreads();
+    if (tid < c.dk) {
+      const unsigned char* vp = c.v_block(page, kv) + tid * PG_TOK;
+      const int n = min(PG_TOK, len - col * PG_TOK);
+      float t = 0.f;
+      for (int u = 0; u < n; ++u) t += p_s[u] * code8<FMT>::load(vp[u]);
+      acc = acc * alpha_s + t * c.v_scale[(size_t)page * c.Hkv + kv];
+    }
+    __syncthreads();
+  }
+  if (tid == 0) alpha_s = l_run == 0.f ? 0.f : 1.f / l_run;   // (NaN stays NaN)
+  __syncthreads();
+  if (tid < c.dk) elem<O>::store(out + ((size_t)b * H + h) * c.dk + tid, acc * alpha_s);
+}
+
+}  // namespace lisa

@@ -152,6 +152,10 @@ int check_launch() {
   return e == hipSuccess ? LISA_OK : hip_fail(e);
 }
 
+int check_common_desc(const lisa_desc* d) { return check_common(d); }
+int check_lisa_desc(const lisa_desc* d) { return check_lisa(d); }
+void note_path(const char* name) { g_path = name; }
+
 StageScope::StageScope(const char* name, hipStream_t s) : st(s) {
   if (!g_prof_on || g_prof_recs.size() >= kMaxProfRecs) return;
   rec.beg = prof_event();
@@ -1269,6 +1273,9 @@ size_t lisa_workspace_bytes(const lisa_desc* desc, int which) {
     case LISA_WS_KD:
       if (check_common(desc) != LISA_OK) return 0;
       return (size_t)kd_blocks(desc) * sizeof(double);
+    case LISA_WS_DECODE8:
+    case LISA_WS_STD_DECODE8:
+      return decode8_bytes(desc, which == LISA_WS_DECODE8);
     default:
       return 0;
   }

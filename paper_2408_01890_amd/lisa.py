@@ -22,7 +22,7 @@ LIB_PATH = os.path.join(_HERE, "liblisa_mi355x.so")
 F32, BF16 = 0, 1
 MIX_ADD, MIX_CONCAT, MIX_PLUS, MIX_SHARE = 0, 1, 2, 3
 ACT_RELU, ACT_SILU, ACT_SINGLE = 0, 1, 2
-WS_PREFILL, WS_DECODE, WS_STD, WS_LAYER, WS_LAYER_DECODE, WS_KD = 0, 1, 2, 3, 4, 5
+WS_PREFILL, WS_DECODE, WS_STD, WS_LAYER, WS_LAYER_DECODE, WS_KD, WS_DECODE8, WS_STD_DECODE8 = range(8)
 
 EXPORTS = (
     "lisa_attn_prefill", "lisa_attn_decode", "std_attn_scores", "lisa_workspace_bytes",
@@ -32,7 +32,8 @@ EXPORTS = (
     "lisa_layer_offsets", "lisa_layer_decode", "lisa_tune_set", "lisa_attn_decode_static",
     "lisa_decode_stack", "lisa_stack_workspace_bytes", "lisa_scores_elems", "lisa_kd_huber",
     "lisa_probe_hbm_read", "lisa_probe_hbm_write", "lisa_probe_mfma", "lisa_launch_choice",
-    "lisa_project_choice",
+    "lisa_project_choice", "lisa_cache8_append", "lisa_attn_decode8", "std_attn_decode8", "lisa_pages_workspace_bytes",
+    "lisa_pages_grow", "lisa_pages_fork", "lisa_pages_free", "lisa_pages_compact", "lisa_pages_copy",
 )
 CHOICE_STD_ORDER, CHOICE_PREFILL = 0, 1
 TUNE_PREFILL_GROUPS, TUNE_PREFILL_SPLIT, TUNE_PREFILL_PAIR, TUNE_STD_PAIR, TUNE_PROJECT_TN, TUNE_PREFILL_SLICES = range(6)
@@ -74,6 +75,21 @@ class StackLayer(C.Structure):
     _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("q", C.c_void_p), ("k_cache", C.c_void_p),
                 ("v_cache", C.c_void_p), ("w1", C.c_void_p), ("w2", C.c_void_p), ("out", C.c_void_p),
                 ("score_row", C.c_void_p)]
+
+
+class Cache8Desc(C.Structure):
+    _fields_ = [
+        ("format", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("Hkv", C.c_int32),
+        ("width", C.c_int32), ("d_k", C.c_int32), ("k", C.c_void_p), ("k_scale", C.c_void_p),
+        ("v", C.c_void_p), ("v_scale", C.c_void_p), ("table", C.c_void_p), ("lens", C.c_void_p),
+    ]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [
+        ("n_pages", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("reserved", C.c_int32),
+        ("table", C.c_void_p), ("lens", C.c_void_p), ("refs", C.c_void_p),
+    ]
 
 
 class StageTime(C.Structure):
@@ -147,6 +163,25 @@ def _lib():
         h.lisa_project_choice.restype = C.c_int
         h.lisa_tune_set.argtypes = [C.c_int, C.c_int]
         h.lisa_tune_set.restype = C.c_int
+        cp, pp = C.POINTER(Cache8Desc), C.POINTER(PagesDesc)
+        h.lisa_cache8_append.argtypes = [dp, cp] + [vp] * 4
+        h.lisa_cache8_append.restype = C.c_int
+        h.lisa_attn_decode8.argtypes = [dp, cp] + [vp] * 7 + [sz, vp]
+        h.lisa_attn_decode8.restype = C.c_int
+        h.std_attn_decode8.argtypes = [dp, cp] + [vp] * 4 + [sz, vp]
+        h.std_attn_decode8.restype = C.c_int
+        h.lisa_pages_workspace_bytes.argtypes = [pp]
+        h.lisa_pages_workspace_bytes.restype = sz
+        h.lisa_pages_grow.argtypes = [pp, vp, vp, vp, sz, vp]
+        h.lisa_pages_grow.restype = C.c_int
+        h.lisa_pages_fork.argtypes = [pp, vp, vp, C.c_int32, vp, vp, vp, sz, vp]
+        h.lisa_pages_fork.restype = C.c_int
+        h.lisa_pages_free.argtypes = [pp, vp, C.c_int32, vp, vp, sz, vp]
+        h.lisa_pages_free.restype = C.c_int
+        h.lisa_pages_compact.argtypes = [pp, vp, vp, sz, vp]
+        h.lisa_pages_compact.restype = C.c_int
+        h.lisa_pages_copy.argtypes = [cp, C.c_int32, vp, C.c_int32, vp]
+        h.lisa_pages_copy.restype = C.c_int
         h.lisa_profile_collect.argtypes = [C.POINTER(StageTime), C.c_int]
         h.lisa_profile_collect.restype = C.c_int
         _handle = h
@@ -728,3 +763,234 @@ class DecodeStack:
         if rc:
             raise LisaError(rc, "lisa_decode_stack")
         return self.outs
+
+
+# ---- the paged 8-bit cache ------------------------------------------------------------------------
+PAGE_TOKENS = 64
+_FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+
+
+def _on(device, **tensors):
+    """Raises ValueError unless the tensors that are given lie on `device` and that is the current one (the streams are its)."""
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name}: on {t.device}, the cache on {device}")
+    if device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"the cache is on {device}, which is not the current device")
+
+
+class Pages:
+    """Which pages of the 8-bit caches the sequences of a server have (lisa_pages in include/lisa.h): `table`
+    [n_seqs, max_pages], `lens` [n_seqs] and `refs` [n_pages], int32 device tensors that the caller owns and the lisa_pages_*
+    calls change in place.  All layers' caches share one."""
+
+    def __init__(self, table, lens, refs):
+        if table.dim() != 2 or table.numel() == 0 or refs.dim() != 1 or refs.numel() == 0:
+            raise ValueError("table is [n_seqs, max_pages], refs [n_pages]")
+        self.n_seqs, self.max_pages = table.shape
+        self.n_pages = refs.shape[0]
+        self.table, self.lens, self.refs, self.device = table, lens, refs, table.device
+        self._desc = PagesDesc(self.n_pages, self.n_seqs, self.max_pages, 0, _ptr(table, "table", dtype=torch.int32),
+                               _ptr(lens, "lens", (self.n_seqs,), torch.int32), _ptr(refs, "refs", dtype=torch.int32))
+        if lens.device != self.device or refs.device != self.device:
+            raise ValueError("table, lens and refs lie on one device")
+        self._ref = C.byref(self._desc)
+        self._need = int(_lib().lisa_pages_workspace_bytes(self._ref))
+        if self._need == 0:
+            raise LisaError(-3, "Pages")
+
+    @classmethod
+    def empty(cls, n_pages, n_seqs, max_pages, device="cuda"):
+        """All sequences empty, all pages free."""
+        return cls(torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(n_seqs, dtype=torch.int32, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device))
+
+
+class Cache8:
+    """A layer's paged 8-bit cache (lisa_cache8 in include/lisa.h) of the sequences of `pages`: k [n_pages,Hkv,ceil(width/8),64,8],
+    v [n_pages,Hkv,d_k,64] (torch.int8 or torch.float8_e4m3fn), k_scale, v_scale [n_pages,Hkv] float32.  `width`: r for K_LR, d_k
+    for the keys of a standard layer, 0 where there are none (k, k_scale are None: a direct-sharing layer)."""
+
+    def __init__(self, pages, k, k_scale, v, v_scale, width):
+        if v.dim() != 4 or v.shape[3] != PAGE_TOKENS or v.dtype not in _FORMATS:
+            raise ValueError("v: expected [n_pages, Hkv, d_k, 64] codes, torch.int8 or torch.float8_e4m3fn")
+        P, Hkv, dk, _ = v.shape
+        if P != pages.n_pages:
+            raise ValueError(f"v: {P} pages, {pages.n_pages} in the page state")
+        if (width == 0) != (k is None) or (k is None) != (k_scale is None):
+            raise ValueError("k and k_scale go with a width of at least 1")
+        self.pages, self.k, self.k_scale, self.v, self.v_scale = pages, k, k_scale, v, v_scale
+        self.Hkv, self.width, self.d_k, self.device = Hkv, width, dk, v.device
+        for name, t in (("k", k), ("k_scale", k_scale), ("v_scale", v_scale), ("table", pages.table)):
+            if t is not None and t.device != self.device:
+                raise ValueError(f"{name}: on {t.device}, v on {self.device}")
+        self._desc = Cache8Desc(_FORMATS[v.dtype], P, pages.max_pages, Hkv, width, dk,
+                                _ptr(k, "k", (P, Hkv, -(-width // 8), PAGE_TOKENS, 8), v.dtype),
+                                _ptr(k_scale, "k_scale", (P, Hkv), torch.float32), _ptr(v, "v"),
+                                _ptr(v_scale, "v_scale", (P, Hkv), torch.float32), pages._desc.table, pages._desc.lens)
+        self._ref = C.byref(self._desc)
+
+    @classmethod
+    def empty(cls, pages, Hkv, width, d_k, format=torch.int8):
+        """A cache of zeros."""
+        z = lambda shape, dt: torch.zeros(shape, dtype=torch.uint8 if dt == format else dt, device=pages.device).view(dt)  # noqa: E731
+        P = pages.n_pages
+        k = z((P, Hkv, -(-width // 8), PAGE_TOKENS, 8), format) if width else None
+        return cls(pages, k, z((P, Hkv), torch.float32) if width else None, z((P, Hkv, d_k, PAGE_TOKENS), format),
+                   z((P, Hkv), torch.float32), width)
+
+
+def _sequences(cache, B):
+    if B > cache.pages.n_seqs:
+        raise ValueError(f"{B} sequences, {cache.pages.n_seqs} in the page state")
+
+
+def lisa_cache8_append(cache, k_new, v_new, *, counts=None):
+    """Stores the last counts[b] (int32 [B], default L) of the pages.lens[b] tokens of sequences 0 .. B-1: k_new [B,Hkv,L,width] (None:
+    width 0), v_new [B,Hkv,L,d_k], row i is token lens[b] - counts[b] + i.  Returns the cache."""
+    B, _, L, _ = v_new.shape
+    dt = v_new.dtype
+    _sequences(cache, B)
+    _on(cache.device, k_new=k_new, v_new=v_new, counts=counts)
+    if cache.width and k_new is None:
+        raise ValueError("k_new: the cache has keys")
+    desc, _ = _plan(None, dt, B, cache.Hkv, cache.Hkv, L, L, cache.d_k, cache.width, 0, MIX_ADD, ACT_RELU, 0.0, 0.0, 0)
+    rc = _lib().lisa_cache8_append(
+        desc, cache._ref, _ptr(k_new if cache.width else None, "k_new", (B, cache.Hkv, L, cache.width), dt),
+        _ptr(v_new, "v_new", (B, cache.Hkv, L, cache.d_k), dt), _ptr(counts, "counts", (B,), torch.int32), _stream())
+    if rc:
+        raise LisaError(rc, "lisa_cache8_append")
+    return cache
+
+
+def lisa_attn_decode8(q_lr, cache, score_row_prev, w1, w2, *, mix=MIX_ADD, act=ACT_RELU, write_scores=True, delta_scale=0.0,
+                      out=None, out_dtype=None, score_row_out=None, workspace=None):
+    """lisa_attn_decode over an 8-bit cache that holds the new token: q_lr [B,H,r] (None: MIX_SHARE), score_row_prev [B,H,Lk]
+    with Lk at least the longest of sequences 0 .. B-1 of the cache.  What lies past a sequence's length is neither read nor written.
+    Returns (out [B,H,d_k], score_row_out [B,H,Lk] or None)."""
+    B, H, Lk = score_row_prev.shape
+    r = q_lr.shape[2] if q_lr is not None else 0
+    has_ffn = mix in (MIX_ADD, MIX_CONCAT)
+    Din, F = w1.shape if has_ffn else (0, 0)
+    if not has_ffn:
+        w1 = w2 = None
+    elif act == ACT_SINGLE:
+        w2 = None
+    if has_ffn and Din != (2 * H if mix == MIX_CONCAT else H):
+        raise ValueError(f"w1 has {Din} rows, expected {2 * H if mix == MIX_CONCAT else H}")
+    sdt = score_row_prev.dtype
+    dt = torch.float32 if sdt == torch.float32 else torch.bfloat16
+    odt, of32 = _out_dtype(dt, out.dtype if out is not None else out_dtype)
+    dk = cache.d_k
+    _sequences(cache, B)
+    _on(cache.device, q_lr=q_lr, score_row_prev=score_row_prev, w1=w1, w2=w2, out=out, score_row_out=score_row_out,
+        workspace=workspace)
+    desc, need = _plan(WS_DECODE8, dt, B, H, cache.Hkv, 1, Lk, dk, r, F, mix, act, delta_scale, 0.0, 0, int(write_scores), 0, 0,
+                       of32)
+    if out is None:
+        out = torch.empty((B, H, dk), dtype=odt, device=cache.device)
+    if write_scores and score_row_out is None:
+        score_row_out = torch.empty((B, H, Lk), dtype=sdt, device=cache.device)
+    if need == 0:
+        raise LisaError(_supported(desc) or -2, "lisa_attn_decode8")
+    workspace, wp, wb = _workspace(need, cache.v, workspace)
+    rc = _lib().lisa_attn_decode8(
+        desc, cache._ref, _ptr(q_lr, "q_lr", (B, H, r), dt),
+        _ptr(score_row_prev, "score_row_prev", (B, H, Lk), score_dtype(dt)), _ptr(w1, "w1", (Din, F), dt),
+        _ptr(w2, "w2", (F, H), dt), _ptr(out, "out", (B, H, dk), odt),
+        _ptr(score_row_out if write_scores else None, "score_row_out", (B, H, Lk), sdt), wp, wb, _stream())
+    if rc:
+        raise LisaError(rc, "lisa_attn_decode8")
+    return out, (score_row_out if write_scores else None)
+
+
+def std_attn_decode8(q, cache, Lk, *, want_scores=True, std_scale=0.0, score_row_out=None, out=None, out_dtype=None,
+                     workspace=None):
+    """std_attn_decode over an 8-bit cache that holds the new token: q [B,H,d_k], Lk at least the longest of sequences
+    0 .. B-1 of the cache (the width of the score rows).  Returns (score row [B,H,Lk] or None, out [B,H,d_k])."""
+    B, H, dk = q.shape
+    dt = q.dtype
+    odt, of32 = _out_dtype(dt, out.dtype if out is not None else out_dtype)
+    _sequences(cache, B)
+    _on(cache.device, q=q, out=out, score_row_out=score_row_out, workspace=workspace)
+    desc, need = _plan(WS_STD_DECODE8, dt, B, H, cache.Hkv, 1, Lk, dk, 0, 0, MIX_ADD, ACT_RELU, 0.0, std_scale, 0, 0, 0, 0, of32)
+    sdt = score_dtype(dt)
+    if want_scores and score_row_out is None:
+        score_row_out = torch.empty((B, H, Lk), dtype=sdt, device=cache.device)
+    if out is None:
+        out = torch.empty((B, H, dk), dtype=odt, device=cache.device)
+    workspace, wp, wb = _workspace(need, cache.v, workspace)
+    rc = _lib().std_attn_decode8(
+        desc, cache._ref, _ptr(q, "q", dtype=dt),
+        _ptr(score_row_out if want_scores else None, "score_row_out", (B, H, Lk), sdt),
+        _ptr(out, "out", (B, H, dk), odt), wp, wb, _stream())
+    if rc:
+        raise LisaError(rc, "std_attn_decode8")
+    return (score_row_out if want_scores else None), out
+
+
+def _pages_call(name, pages, workspace, *args, **tensors):
+    _on(pages.device, workspace=workspace, **tensors)
+    workspace, wp, wb = _workspace(pages._need, pages.table, workspace)
+    rc = getattr(_lib(), name)(pages._ref, *args, wp, wb, _stream())
+    if rc:
+        raise LisaError(rc, name)
+
+
+def lisa_pages_grow(pages, add, *, done=None, workspace=None):
+    """Gives sequence s add[s] (int32 [n_seqs]) more tokens and the pages they need.  Returns done [n_seqs] int32: 0 where a
+    sequence is as it was, for lack of room."""
+    if done is None:
+        done = torch.empty(pages.n_seqs, dtype=torch.int32, device=pages.device)
+    _pages_call("lisa_pages_grow", pages, workspace, _ptr(add, "add", (pages.n_seqs,), torch.int32),
+                _ptr(done, "done", (pages.n_seqs,), torch.int32), add=add, done=done)
+    return done
+
+
+def lisa_pages_fork(pages, src, dst, *, done=None, copies=None, workspace=None):
+    """Makes the empty sequences dst (int32 [n]) what the sequences src are.  Returns (done [n], copies [n, 2]): the pages that
+    lisa_pages_copy has to copy in every layer before the next append."""
+    n = src.shape[0]
+    if done is None:
+        done = torch.empty(n, dtype=torch.int32, device=pages.device)
+    if copies is None:
+        copies = torch.empty((n, 2), dtype=torch.int32, device=pages.device)
+    _pages_call("lisa_pages_fork", pages, workspace, _ptr(src, "src", (n,), torch.int32), _ptr(dst, "dst", (n,), torch.int32), n,
+                _ptr(done, "done", (n,), torch.int32), _ptr(copies, "copies", (n, 2), torch.int32), src=src, dst=dst, done=done,
+                copies=copies)
+    return done, copies
+
+
+def lisa_pages_free(pages, seqs, *, done=None, workspace=None):
+    """Empties the sequences seqs (int32 [n]).  Returns done [n] int32."""
+    n = seqs.shape[0]
+    if done is None:
+        done = torch.empty(n, dtype=torch.int32, device=pages.device)
+    _pages_call("lisa_pages_free", pages, workspace, _ptr(seqs, "seqs", (n,), torch.int32), n,
+                _ptr(done, "done", (n,), torch.int32), seqs=seqs, done=done)
+    return done
+
+
+def lisa_pages_compact(pages, *, copies=None, workspace=None):
+    """Moves the used pages to the front of the pool in the page state.  Returns copies [n_pages // 2, 2], which lisa_pages_copy has
+    to copy in every layer before anything else uses the caches."""
+    if copies is None:
+        copies = torch.empty((pages.n_pages // 2, 2), dtype=torch.int32, device=pages.device)
+    _pages_call("lisa_pages_compact", pages, workspace, _ptr(copies, "copies", (pages.n_pages // 2, 2), torch.int32),
+                copies=copies)
+    return copies
+
+
+def lisa_pages_copy(caches, copies):
+    """Copies pages copies[:, 0] of every cache in `caches` to pages copies[:, 1] (pairs of -1: nothing)."""
+    caches = list(caches)
+    if not caches or copies.shape[0] == 0:
+        return
+    for c in caches:
+        _on(c.device, copies=copies)
+    arr = (Cache8Desc * len(caches))(*[c._desc for c in caches])
+    rc = _lib().lisa_pages_copy(arr, len(caches), _ptr(copies, "copies", (copies.shape[0], 2), torch.int32), copies.shape[0],
+                                _stream())
+    if rc:
+        raise LisaError(rc, "lisa_pages_copy")
