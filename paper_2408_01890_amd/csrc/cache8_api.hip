@@ -5,6 +5,14 @@
 
 using namespace lisa;
 
+namespace lisa {
+// launch_cache8.hip
+bool cache8_fast_ok(const lisa_desc* d, bool lisa_layer);
+size_t cache8_fast_bytes(const lisa_desc* d, bool lisa_layer);
+int run_cache8_fast(const lisa_desc* d, bool lisa_layer, int fmt, const Cache8View& c, const void* q, const void* prev, const void* w1,
+                    const void* w2, float scale, void* row, void* out, void* workspace, hipStream_t st);
+}  // namespace lisa
+
 namespace {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -92,7 +100,9 @@ int run_generic(const lisa_desc* d, const Cache8View& c, const void* q, const vo
 int run_decode8(const lisa_desc* d, const lisa_cache8* cache, const void* q, const void* prev, const void* w1, const void* w2, int mix,
                 float scale, void* scores, void* out, void* workspace, hipStream_t st) {
   const Cache8View c = view(cache);
-  const bool e4m3 = cache->format == LISA_CACHE_E4M3;
+  const bool e4m3 = cache->format == LISA_CACHE_E4M3, lisa_layer = mix != 4;
+  if (cache8_fast_ok(d, lisa_layer))
+    return run_cache8_fast(d, lisa_layer, e4m3, c, q, prev, w1, w2, scale, scores, out, workspace, st);
   auto run = d->dtype == LISA_F32 ? (e4m3 ? run_generic<float, float, 1> : run_generic<float, float, 0>)
                                   : (e4m3 ? run_generic<bf16_t, half_t, 1> : run_generic<bf16_t, half_t, 0>);
   return run(d, c, q, prev, w1, w2, mix, scale, scores, out, workspace, st);
@@ -133,7 +143,8 @@ int pages_done() {
 
 namespace lisa {
 size_t decode8_bytes(const lisa_desc* d, bool lisa_layer) {
-  return check_decode8(d, lisa_layer) == LISA_OK ? generic_bytes(d) : 0;
+  if (check_decode8(d, lisa_layer) != LISA_OK) return 0;
+  return cache8_fast_ok(d, lisa_layer) ? cache8_fast_bytes(d, lisa_layer) : generic_bytes(d);
 }
 }  // namespace lisa
 

@@ -1,0 +1,266 @@
+// Decode steps over the paged 8-bit cache on the matrix cores (kernels_cache8_mfma.h): which calls take that way, their
+// workspace, their launches.  LISA_PART 0 .. 3: the scores kernels (ADD and CONCAT, ReLU and SiLU); 4, 5: softmax and P V by format; 6: the rest.
+#include "host.h"
+#include "kernels_cache8_mfma.h"
+
+namespace lisa {
+
+namespace {
+template <int HBI, int FS, int HBO, int ACT, int MODE, int KS>
+int launch_scores_t(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
+  const int lds = cache8_scores_lds(d->H, KS, MODE == 0 ? 0 : MfmaFfn<HBI, FS, HBO, ACT>::kStageBytes);
+  auto kern = k_cache8_scores_mfma<HBI, FS, HBO, ACT, MODE, KS>;
+  if (lds > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return hip_fail(e);
+  }
+  StageScope prof("k_cache8_scores_mfma", st);
+  kern<<<dim3((d->Lk + PG_TOK - 1) / PG_TOK, d->B), 256, lds, st>>>(a);
+  return check_launch();
+}
+template <int HBI, int FS, int HBO, int ACT, int MODE>
+int launch_scores_ks(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
+  return a.c.w <= 32 ? launch_scores_t<HBI, FS, HBO, ACT, MODE, 1>(d, a, st) : launch_scores_t<HBI, FS, HBO, ACT, MODE, 2>(d, a, st);
+}
+template <int HB, int ACT>
+int launch_add_fs(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
+  switch ((a.F + 31) / 32) {
+    case 1: return launch_scores_ks<HB, 1, HB, ACT, 1>(d, a, st);
+    case 2: return launch_scores_ks<HB, 2, HB, ACT, 1>(d, a, st);
+    case 3: return launch_scores_ks<HB, 3, HB, ACT, 1>(d, a, st);
+    default: return launch_scores_ks<HB, 4, HB, ACT, 1>(d, a, st);
+  }
+}
+template <int HBI, int HBO, int ACT>
+int launch_concat_fs(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
+  if (a.F <= 64) return launch_scores_ks<HBI, 2, HBO, ACT, 2>(d, a, st);
+  if (a.F <= 128) return launch_scores_ks<HBI, 4, HBO, ACT, 2>(d, a, st);
+  return launch_scores_ks<HBI, 8, HBO, ACT, 2>(d, a, st);
+}
+}  // namespace
+
+template <int ACT>
+int launch_cache8_add(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st);
+template <int ACT>
+int launch_cache8_concat(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st);
+template <int FMT>
+int launch_cache8_pv(const lisa_desc* d, int mode, int wide, const Cache8PvArgs& a, hipStream_t st);
+
+#if LISA_PART <= 1
+template <int ACT>
+int launch_cache8_add(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
+  switch ((d->H + 15) / 16) {
+    case 1: return launch_add_fs<1, ACT>(d, a, st);
+    case 2: return launch_add_fs<2, ACT>(d, a, st);
+    case 3: return launch_add_fs<3, ACT>(d, a, st);
+    default: return launch_add_fs<4, ACT>(d, a, st);
+  }
+}
+template int launch_cache8_add<LISA_PART>(const lisa_desc*, const Cache8ScoresArgs&, hipStream_t);
+#elif LISA_PART <= 3
+template <int ACT>
+int launch_cache8_concat(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
+  return d->H <= 16 ? launch_concat_fs<2, 1, ACT>(d, a, st) : d->H <= 32 ? launch_concat_fs<4, 2, ACT>(d, a, st) : launch_concat_fs<6, 3, ACT>(d, a, st);
+}
+template int launch_cache8_concat<LISA_PART - 2>(const lisa_desc*, const Cache8ScoresArgs&, hipStream_t);
+#elif LISA_PART <= 5
+namespace {
+template <int FMT, int DK, int MODE, int GT, int GH>
+int launch_pv_nw(const lisa_desc* d, int wide, const Cache8PvArgs& a, hipStream_t st) {
+  const dim3 grid(d->Hkv * a.chunks, a.n_span, d->B);
+  StageScope prof("k_cache8_pv", st);
+  if (wide) k_cache8_pv<FMT, DK, MODE, GT, GH, 8><<<grid, 512, 0, st>>>(a);
+  else k_cache8_pv<FMT, DK, MODE, GT, GH, 4><<<grid, 256, 0, st>>>(a);
+  return check_launch();
+}
+template <int FMT, int DK, int MODE>
+int launch_pv_heads(const lisa_desc* d, int wide, const Cache8PvArgs& a, hipStream_t st) {
+  const int group = d->H / d->Hkv;
+  if (group == 1) return launch_pv_nw<FMT, DK, MODE, 1, 1>(d, wide, a, st);
+  if (group <= 4) return launch_pv_nw<FMT, DK, MODE, 1, 4>(d, wide, a, st);
+  return launch_pv_nw<FMT, DK, MODE, 2, 4>(d, wide, a, st);
+}
+template <int FMT, int DK>
+int launch_pv_mode(const lisa_desc* d, int mode, int wide, const Cache8PvArgs& a, hipStream_t st) {
+  return mode == 0   ? launch_pv_heads<FMT, DK, 0>(d, wide, a, st)
+         : mode == 1 ? launch_pv_heads<FMT, DK, 1>(d, wide, a, st)
+                     : launch_pv_heads<FMT, DK, 2>(d, wide, a, st);
+}
+}  // namespace
+template <int FMT>
+int launch_cache8_pv(const lisa_desc* d, int mode, int wide, const Cache8PvArgs& a, hipStream_t st) {
+  return d->d_k == 128 ? launch_pv_mode<FMT, 128>(d, mode, wide, a, st) : launch_pv_mode<FMT, 64>(d, mode, wide, a, st);
+}
+template int launch_cache8_pv<LISA_PART - 4>(const lisa_desc*, int, int, const Cache8PvArgs&, hipStream_t);
+#else
+
+namespace {
+
+// The module that the scores kernel runs: a single layer y = W^T x is the ReLU network [W, -W], [I; -I] (k_synth_relu_ffn).
+struct Module {
+  int Din, F, act, mix;
+};
+Module module_of(const lisa_desc* d) {
+  Module m;
+  m.mix = d->mix;
+  m.Din = d->mix == LISA_MIX_CONCAT ? 2 * d->H : d->H;
+  m.F = d->act == LISA_ACT_SINGLE ? 2 * d->H : d->F;
+  m.act = d->act == LISA_ACT_SILU ? 1 : 0;
+  return m;
+}
+FfnOperands operand_shape(const lisa_desc* d) {              // (the instantiation that is launched)
+  const Module m = module_of(d);
+  const bool concat = m.mix == LISA_MIX_CONCAT;
+  FfnOperands w{};
+  w.Din = m.Din;
+  w.F = m.F;
+  w.HO = d->H;
+  w.HBO = concat ? (d->H <= 16 ? 1 : d->H <= 32 ? 2 : 3) : (d->H + 15) / 16;
+  w.KS = concat ? w.HBO : (w.HBO + 1) / 2;
+  w.FS = !concat ? (m.F + 31) / 32 : m.F <= 64 ? 2 : m.F <= 128 ? 4 : 8;
+  return w;
+}
+__global__ __launch_bounds__(256) void k_cache8_operands(FfnOperands w) { ffn_operand_piece<false>(w, blockIdx.x * 256 + threadIdx.x); }
+
+// Softmax and P V: eight waves per workgroup where two pages each makes all pages of a sequence one workgroup's work, or four with as many
+// pages each as make some 4096 waves of the call (16 per compute unit).
+struct PvGeom {
+  int wide, span_pages, n_span, chunks;
+};
+PvGeom pv_geom(const lisa_desc* d) {
+  const int group = d->H / d->Hkv, n_pages = (d->Lk + PG_TOK - 1) / PG_TOK;
+  PvGeom g;
+  g.chunks = group <= 4 ? 1 : (group + 7) / 8;
+  const long long base = (long long)d->B * d->Hkv * g.chunks;
+  const int per_wave = (int)std::min<long long>(64, std::max<long long>(1, base * n_pages / 4096));
+  g.wide = base * ((n_pages + 15) / 16) <= 512 || n_pages <= 16;
+  if (base >= 1024) g.wide = 0;
+  g.span_pages = std::min(g.wide ? std::max(16, 8 * per_wave) : 4 * per_wave, (n_pages + 3) / 4 * 4);
+  g.n_span = (n_pages + g.span_pages - 1) / g.span_pages;
+  return g;
+}
+
+struct Ws {
+  size_t s, part_o, part_ml, img, w1, w2, total;
+  int Lp;
+};
+Ws ws_of(const lisa_desc* d, bool lisa_layer) {
+  const PvGeom g = pv_geom(d);
+  Ws w{};
+  w.Lp = (d->Lk + PG_TOK - 1) / PG_TOK * PG_TOK;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t r = at;
+    at = round_up(at + bytes, 256);
+    return r;
+  };
+  const size_t parts = g.n_span > 1 ? (size_t)d->B * g.n_span * d->H : 0;
+  w.part_o = take(parts * d->d_k * sizeof(float));
+  w.part_ml = take(parts * 2 * sizeof(float));
+  if (lisa_layer && d->mix != LISA_MIX_SHARE) {
+    w.s = take((size_t)d->B * d->H * w.Lp * sizeof(float));
+    if (d->mix != LISA_MIX_PLUS) {
+      w.img = take((size_t)operand_shape(d).pieces() * 16);
+      if (d->act == LISA_ACT_SINGLE) {
+        w.w1 = take((size_t)module_of(d).Din * 2 * d->H * 2);
+        w.w2 = take((size_t)2 * d->H * d->H * 2);
+      }
+    }
+  }
+  w.total = std::max<size_t>(at, 256);
+  return w;
+}
+
+}  // namespace
+
+bool cache8_fast_ok(const lisa_desc* d, bool lisa_layer) {
+  if (d->dtype != LISA_BF16 || (d->d_k != 64 && d->d_k != 128)) return false;
+  if ((long long)(d->H / d->Hkv + 7) / 8 * d->Hkv > 65535) return false;
+  if (!lisa_layer || d->mix == LISA_MIX_SHARE) return true;
+  if (d->r > 64 || d->H > 64) return false;
+  if (d->mix == LISA_MIX_PLUS) return true;
+  const Module m = module_of(d);
+  return d->mix == LISA_MIX_CONCAT ? d->H <= 48 && m.F <= 256 : m.F <= 128;
+}
+
+size_t cache8_fast_bytes(const lisa_desc* d, bool lisa_layer) { return ws_of(d, lisa_layer).total; }
+
+int run_cache8_fast(const lisa_desc* d, bool lisa_layer, int fmt, const Cache8View& c, const void* q, const void* prev, const void* w1,
+                    const void* w2, float scale, void* row, void* out, void* workspace, hipStream_t st) {
+  const Ws w = ws_of(d, lisa_layer);
+  const PvGeom g = pv_geom(d);
+  char* ws = (char*)workspace;
+  const bool share = lisa_layer && d->mix == LISA_MIX_SHARE;
+  if (lisa_layer && !share) {
+    Cache8ScoresArgs a{};
+    a.c = c;
+    a.q = (const bf16_t*)q;
+    a.prev = (const half_t*)prev;
+    a.row = (half_t*)row;
+    a.s = (float*)(ws + w.s);
+    a.H = d->H;
+    a.Lk = d->Lk;
+    a.Lp = w.Lp;
+    a.fmt = fmt;
+    a.scale = scale;
+    int rc;
+    if (d->mix == LISA_MIX_PLUS) {
+      rc = launch_scores_ks<1, 1, 1, 0, 0>(d, a, st);
+    } else {
+      const Module m = module_of(d);
+      if (d->act == LISA_ACT_SINGLE) {
+        StageScope prof("k_synth_relu_ffn", st);
+        k_synth_relu_ffn<bf16_t><<<(2 * m.Din * d->H + 2 * d->H * d->H + 255) / 256, 256, 0, st>>>(
+            (const bf16_t*)w1, (bf16_t*)(ws + w.w1), (bf16_t*)(ws + w.w2), m.Din, d->H);
+        w1 = ws + w.w1;
+        w2 = ws + w.w2;
+      }
+      FfnOperands o = operand_shape(d);
+      o.w1 = (const bf16_t*)w1;
+      o.w2 = (const bf16_t*)w2;
+      o.out = (unsigned short*)(ws + w.img);
+      {
+        StageScope prof("k_cache8_operands", st);
+        k_cache8_operands<<<(o.pieces() + 255) / 256, 256, 0, st>>>(o);
+        rc = check_launch();
+        if (rc) return rc;
+      }
+      a.img = o.out;
+      a.F = m.F;
+      rc = d->mix == LISA_MIX_CONCAT ? (m.act ? launch_cache8_concat<1>(d, a, st) : launch_cache8_concat<0>(d, a, st))
+                                     : (m.act ? launch_cache8_add<1>(d, a, st) : launch_cache8_add<0>(d, a, st));
+    }
+    if (rc) return rc;
+  }
+  Cache8PvArgs p{};
+  p.c = c;
+  p.q = (const bf16_t*)q;
+  p.s = (const float*)(ws + w.s);
+  p.prev = (const half_t*)prev;
+  p.row = lisa_layer && !share ? nullptr : (half_t*)row;
+  p.out = out;
+  p.part_o = (float*)(ws + w.part_o);
+  p.part_ml = (float*)(ws + w.part_ml);
+  p.H = d->H;
+  p.Lk = d->Lk;
+  p.Lp = w.Lp;
+  p.n_span = g.n_span;
+  p.span_pages = g.span_pages;
+  p.chunks = g.chunks;
+  p.out_f32 = d->out_f32;
+  p.scale = scale;
+  const int mode = !lisa_layer ? 0 : share ? 2 : 1;
+  int rc = fmt ? launch_cache8_pv<1>(d, mode, g.wide, p, st) : launch_cache8_pv<0>(d, mode, g.wide, p, st);
+  if (rc) return rc;
+  if (g.n_span > 1) {
+    StageScope prof("k_cache8_combine", st);
+    auto kern = d->d_k == 128 ? k_cache8_combine<128> : k_cache8_combine<64>;
+    kern<<<dim3(d->H, d->B), d->d_k, 0, st>>>(p.part_o, p.part_ml, c.lens, out, d->H, d->Lk, g.n_span, g.span_pages * PG_TOK, d->out_f32);
+    rc = check_launch();
+  }
+  if (rc == LISA_OK) note_path("decode8");
+  return rc;
+}
+#endif
+
+}  // namespace lisa
