@@ -108,6 +108,14 @@ int run_decode8(const lisa_desc* d, const lisa_cache8* cache, const void* q, con
   return run(d, c, q, prev, w1, w2, mix, scale, scores, out, workspace, st);
 }
 
+template <typename T>
+void launch_append(const Cache8View& c, bool e4m3, dim3 grid, const void* k_new, const void* v_new, const int32_t* counts, int L, hipStream_t st) {
+  const bool wide = c.w > 128 || c.dk > 128;
+  auto kern = e4m3 ? (wide ? k_cache8_append<T, 1, true> : k_cache8_append<T, 1, false>)
+                   : (wide ? k_cache8_append<T, 0, true> : k_cache8_append<T, 0, false>);
+  kern<<<grid, 256, 0, st>>>(c, (const T*)k_new, (const T*)v_new, counts, L);
+}
+
 // ---- pages ------------------------------------------------------------------------------------
 int check_pages(const lisa_pages* p) {
   if (!p) return LISA_ERR_NULL;
@@ -166,13 +174,9 @@ int lisa_cache8_append(const lisa_desc* d, const lisa_cache8* cache, const void*
   const Cache8View c = view(cache);
   const dim3 grid((unsigned)(((long long)d->Lq + 126) / 64), d->Hkv, d->B);
   StageScope prof("k_cache8_append", st);
-  if (d->dtype == LISA_F32) {
-    auto kern = cache->format == LISA_CACHE_E4M3 ? k_cache8_append<float, 1> : k_cache8_append<float, 0>;
-    kern<<<grid, 256, 0, st>>>(c, (const float*)k_new, (const float*)v_new, counts, d->Lq);
-  } else {
-    auto kern = cache->format == LISA_CACHE_E4M3 ? k_cache8_append<bf16_t, 1> : k_cache8_append<bf16_t, 0>;
-    kern<<<grid, 256, 0, st>>>(c, (const bf16_t*)k_new, (const bf16_t*)v_new, counts, d->Lq);
-  }
+  const bool e4m3 = cache->format == LISA_CACHE_E4M3;
+  if (d->dtype == LISA_F32) launch_append<float>(c, e4m3, grid, k_new, v_new, counts, d->Lq, st);
+  else launch_append<bf16_t>(c, e4m3, grid, k_new, v_new, counts, d->Lq, st);
   rc = check_launch();
   if (rc == LISA_OK) note_path("cache8_append");
   return rc;

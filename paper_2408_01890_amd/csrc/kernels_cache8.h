@@ -72,14 +72,59 @@ struct Cache8View {
 };
 
 // ---- append -----------------------------------------------------------------------------------
+// Eight features f0 .. f0 + 7 of a row of `width` elements (zeros past the width).  Rows of whole octets are 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void load_octet(const T* row, int f0, int width, float (&x)[8]) {
+  typedef unsigned int u32x4_ __attribute__((ext_vector_type(4)));
+  if constexpr (sizeof(T) == 4) {
+    if (width % 8 == 0) {
+      const float4 a = *(const float4*)(row + f0), b = *(const float4*)(row + f0 + 4);
+      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+      return;
+    }
+  } else {
+    if (width % 8 == 0) {
+      const u32x4_ a = *(const u32x4_*)(row + f0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[2 * i] = bf16_bits_to_f32(a[i] & 0xffffu), x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+      return;
+    }
+    if (width % 2 == 0) {                                    // (rows are 4-byte aligned)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned a = f0 + 2 * i < width ? *(const unsigned*)(row + f0 + 2 * i) : 0u;
+        x[2 * i] = bf16_bits_to_f32(a & 0xffffu), x[2 * i + 1] = __uint_as_float(a & 0xffff0000u);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = f0 + i < width ? elem<T>::load(row + f0 + i) : 0.f;
+}
+__device__ __forceinline__ float octet_max(const float (&x)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(x[i]));
+  return m;
+}
+template <int FMT>
+__device__ __forceinline__ unsigned long long octet_codes(const float (&x)[8], float inv) {
+  unsigned long long y = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y |= (unsigned long long)code8<FMT>::store(x[i] * inv) << (8 * i);
+  return y;
+}
+
 // The last counts[b] tokens of sequence b (all L rows where counts is null) go into its pages.
-// grid (pages that L tokens can touch, Hkv, B), block 256: a workgroup has one page of one head: the largest
-// magnitudes of its new keys and values, the scales, then the codes; values are turned through the LDS into rows of tokens.
+// grid (pages that L tokens can touch, Hkv, B), block 256: a workgroup has one page of one head.  Its new rows are read once, into
+// registers (a thread: eight features of four tokens), for the largest magnitudes and then the codes; values are turned
+// through the LDS into rows of tokens.  WIDE: rows of more than 128 features.
 constexpr int C8_VROW = PG_TOK + 4;      // bytes of a feature's row of codes in the LDS
-template <typename T, int FMT>
+template <typename T, int FMT, bool WIDE>
 __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __restrict__ k_new, const T* __restrict__ v_new,
                                                        const int* __restrict__ counts, int L) {
-  __shared__ __align__(16) unsigned char v_s[256 * C8_VROW];
+  constexpr int N = WIDE ? 2 : 1, FEATURES = N * 128;        // (16 token quads x width / 8 tasks for N * 256 threads)
+  __shared__ __align__(16) unsigned char v_s[FEATURES * C8_VROW];
   __shared__ float m_s[2][4];
   const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int len = c.lens[b], n_new = min(max(counts ? counts[b] : L, 0), min(L, len));
@@ -88,18 +133,50 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __
   if ((long long)col * PG_TOK >= len) return;
   const int page = c.page_of(b, col);
   if (page < 0) return;
-  const int lo = max(len - n_new - col * PG_TOK, 0), hi = min(len - col * PG_TOK, PG_TOK);
-  const size_t row0 = ((size_t)b * c.Hkv + kv) * L + (col * PG_TOK + lo - (len - n_new));
-  const T* ks = k_new + row0 * c.w;
-  const T* vs = v_new + row0 * c.dk;
-  const int n = hi - lo;
-  float mk = 0.f, mv = 0.f;
-  for (int e = tid; e < n * c.w; e += 256) mk = fmaxf(mk, finite_abs(elem<T>::load(ks + e)));
-  for (int e = tid; e < n * c.dk; e += 256) mv = fmaxf(mv, finite_abs(elem<T>::load(vs + e)));
-  mk = wave_max(mk), mv = wave_max(mv);
-  if ((tid & 63) == 0) m_s[0][tid >> 6] = mk, m_s[1][tid >> 6] = mv;
+  const int lo = max(len - n_new - col * PG_TOK, 0), hi = min(len - col * PG_TOK, PG_TOK);   // tokens of the page
   const size_t at = (size_t)page * c.Hkv + kv;
   const float k_old = c.w ? c.k_scale[at] : 0.f, v_old = c.v_scale[at];
+  // row of token t of the page: base + t (t >= lo)
+  const long long base = ((long long)b * c.Hkv + kv) * L + (col * PG_TOK - (len - n_new));
+  const int nv = (c.dk + 7) / 8, nk = c.w8 / 8;
+  const bool k_quads = c.w % 8 == 0;                         // else a thread has a token, three octets at most of a K_LR row keep all busy
+  float xv[N][4][8], xk[N][4][8], mk = 0.f, mv = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = tid + 256 * i, q = e / nv, o = e % nv;     // token quad, octet (octets fastest: rows are read on end)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int t = 4 * q + u;
+#pragma unroll
+      for (int f = 0; f < 8; ++f) xv[i][u][f] = 0.f;
+      if (t >= lo && t < hi) load_octet(v_new + (base + t) * c.dk, 8 * o, c.dk, xv[i][u]);
+      mv = fmaxf(mv, octet_max(xv[i][u]));
+    }
+  }
+  if (k_quads) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = tid + 256 * i, q = nk ? e / nk : 16, o = nk ? e % nk : 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = 4 * q + u;
+#pragma unroll
+        for (int f = 0; f < 8; ++f) xk[i][u][f] = 0.f;
+        if (t >= lo && t < hi) load_octet(k_new + (base + t) * c.w, 8 * o, c.w, xk[i][u]);
+        mk = fmaxf(mk, octet_max(xk[i][u]));
+      }
+    }
+  } else {
+    for (int e = tid; e < 64 * nk; e += 256) {
+      const int t = e & 63;
+      if (t < lo || t >= hi) continue;
+      float x[8];
+      load_octet(k_new + (base + t) * c.w, 8 * (e >> 6), c.w, x);
+      mk = fmaxf(mk, octet_max(x));
+    }
+  }
+  mk = wave_max(mk), mv = wave_max(mv);
+  if ((tid & 63) == 0) m_s[0][tid >> 6] = mk, m_s[1][tid >> 6] = mv;
   __syncthreads();
   mk = fmaxf(fmaxf(m_s[0][0], m_s[0][1]), fmaxf(m_s[0][2], m_s[0][3]));
   mv = fmaxf(fmaxf(m_s[1][0], m_s[1][1]), fmaxf(m_s[1][2], m_s[1][3]));
@@ -110,19 +187,44 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __
     c.v_scale[at] = v_now;
   }
   typedef code8<FMT> Code;
+  // values: through the LDS, [feature][token]
+  const float v_inv = 1.f / v_now, k_inv = 1.f / k_now;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = tid + 256 * i, q = e / nv, o = e % nv;
+    if (q >= 16 || 4 * q >= hi || 4 * q + 4 <= lo) continue;
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+      unsigned y = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) y |= (unsigned)Code::store(xv[i][u][f] * v_inv) << (8 * u);
+      if (8 * o + f < c.dk) *(unsigned*)(v_s + (8 * o + f) * C8_VROW + 4 * q) = y;
+    }
+  }
   // keys: 8 features of a token at a time
   unsigned char* kb = c.k_block(page, kv);
-  const float k_inv = 1.f / k_now;
-  for (int e = tid; e < n * (c.w8 / 8); e += 256) {
-    const int t = e % n, p = e / n;
-    unsigned long long x = 0;
-    for (int f = 0; f < 8; ++f)
-      if (8 * p + f < c.w)
-        x |= (unsigned long long)Code::store(elem<T>::load(ks + (size_t)t * c.w + 8 * p + f) * k_inv) << (8 * f);
-    *(unsigned long long*)(kb + ((size_t)p * PG_TOK + lo + t) * 8) = x;
+  if (k_quads) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = tid + 256 * i, q = nk ? e / nk : 16, o = nk ? e % nk : 0;
+      if (q >= 16) continue;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = 4 * q + u;
+        if (t >= lo && t < hi) *(unsigned long long*)(kb + (o * PG_TOK + t) * 8) = octet_codes<FMT>(xk[i][u], k_inv);
+      }
+    }
+  } else {
+    for (int e = tid; e < 64 * nk; e += 256) {
+      const int t = e & 63;
+      if (t < lo || t >= hi) continue;
+      float x[8];
+      load_octet(k_new + (base + t) * c.w, 8 * (e >> 6), c.w, x);
+      *(unsigned long long*)(kb + ((e >> 6) * PG_TOK + t) * 8) = octet_codes<FMT>(x, k_inv);
+    }
   }
   if (lo && k_now > k_old)
-    for (int e = tid; e < lo * (c.w8 / 8); e += 256) {
+    for (int e = tid; e < lo * nk; e += 256) {
       unsigned long long* at8 = (unsigned long long*)(kb + ((size_t)(e / lo) * PG_TOK + e % lo) * 8);
       const unsigned long long x = *at8;
       unsigned long long y = 0;
@@ -130,25 +232,24 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __
         y |= (unsigned long long)Code::store(Code::load((unsigned char)(x >> (8 * f))) * k_old * k_inv) << (8 * f);
       *at8 = y;
     }
-  // values: through the LDS, [feature][token]
-  unsigned char* vb = c.v_block(page, kv);
-  const float v_inv = 1.f / v_now;
-  const int from = lo && v_now > v_old ? 0 : lo;              // tokens to write
-  for (int e = tid; e < n * c.dk; e += 256) v_s[(e % c.dk) * C8_VROW + lo + e / c.dk] = Code::store(elem<T>::load(vs + e) * v_inv);
-  for (int e = tid; e < (lo - from) * c.dk; e += 256) {
-    const int f = e / lo, t = e % lo;
-    v_s[f * C8_VROW + t] = Code::store(Code::load(vb[f * PG_TOK + t]) * v_old * v_inv);
-  }
   __syncthreads();
-  for (int e = tid; e < c.dk * 16; e += 256) {               // 4 tokens of a feature at a time
-    const int f = e >> 4, t = 4 * (e & 15);
-    const unsigned x = *(const unsigned*)(v_s + f * C8_VROW + t);
+  unsigned char* vb = c.v_block(page, kv);
+  const int from = lo && v_now > v_old ? 0 : lo;              // tokens to write
+  if (from < lo) {
+    for (int e = tid; e < lo * c.dk; e += 256) {
+      const int f = e / lo, t = e % lo;
+      v_s[f * C8_VROW + t] = Code::store(Code::load(vb[f * PG_TOK + t]) * v_old * v_inv);
+    }
+    __syncthreads();
+  }
+  for (int e = tid; e < c.dk * 4; e += 256) {                // 16 tokens of a feature at a time
+    const int f = e >> 2, t = 16 * (e & 3);
+    const unsigned* src = (const unsigned*)(v_s + f * C8_VROW + t);
     unsigned char* dst = vb + f * PG_TOK + t;
-    if (t >= from && t + 4 <= hi) {
-      *(unsigned*)dst = x;
-    } else {
-      for (int u = 0; u < 4; ++u)
-        if (t + u >= from && t + u < hi) dst[u] = (unsigned char)(x >> (8 * u));
+    if (t >= from && t + 16 <= hi) {
+      *(uint4*)dst = make_uint4(src[0], src[1], src[2], src[3]);
+    } else if (t < hi && t + 16 > from) {
+      for (int u = max(from - t, 0); u < min(hi - t, 16); ++u) dst[u] = ((const unsigned char*)src)[u];
     }
   }
 }

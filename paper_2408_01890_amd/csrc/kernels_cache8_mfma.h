@@ -113,25 +113,25 @@ __device__ __forceinline__ void stage_queries(int H, int n, unsigned char* codes
   }
 }
 
-// Scores of a page against four heads from its keys: x[f] = score of token 16 g + f, head n % 4.
-// kreg[s][u]: 16 bytes of a lane, tokens T and T + 1 (T = 16 (n / 4) + 8 u + 2 (n % 4)), features 32 s + 8 g .. + 7.
-// weight: of this lane's piece, with the scales.
+// Scores of a page against the four heads of a tile: x[f] = score of token 16 g + f, head n % 4.
+// kreg[s][u]: 16 bytes of a lane, tokens T and T + 1 (T = 16 (n / 4) + 8 u + 2 (n % 4)), features 32 s + 8 g .. + 7.  page_products may be
+// called for several key blocks, with zeros in the columns of the heads that do not go with them.
 template <int FMT, int KS>
-__device__ __forceinline__ void page_scores(const c8_u32x4 (&kreg)[KS][2], const unsigned long long (&qc)[KS], float weight, float (&x)[16]) {
-  typedef mfma8<FMT> M;
+__device__ __forceinline__ void page_products(const c8_u32x4 (&kreg)[KS][2], const unsigned long long (&qc)[KS], typename mfma8<FMT>::acc (&acc)[2][2]) {
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    typename M::acc a0 = M::zero(), a1 = M::zero();
+  for (int s = 0; s < KS; ++s)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      a0 = M::mul(kreg[s][u][0] | (unsigned long long)kreg[s][u][1] << 32, qc[s], a0);
-      a1 = M::mul(kreg[s][u][2] | (unsigned long long)kreg[s][u][3] << 32, qc[s], a1);
+    for (int u = 0; u < 2; ++u) {
+      acc[u][0] = mfma8<FMT>::mul(kreg[s][u][0] | (unsigned long long)kreg[s][u][1] << 32, qc[s], acc[u][0]);
+      acc[u][1] = mfma8<FMT>::mul(kreg[s][u][2] | (unsigned long long)kreg[s][u][3] << 32, qc[s], acc[u][1]);
     }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) x[8 * u + 2 * v] = (float)a0[v] * weight, x[8 * u + 2 * v + 1] = (float)a1[v] * weight;
-  }
+}
+// weight: of this lane's piece, with the scales.
+template <int FMT>
+__device__ __forceinline__ void page_sums(const typename mfma8<FMT>::acc (&acc)[2][2], float weight, float (&x)[16]) {
 #pragma unroll
   for (int f = 0; f < 16; ++f) {
+    x[f] = (float)acc[f >> 3][f & 1][(f & 7) >> 1] * weight;
     x[f] += dpp_move<0x128>(x[f]);                           // row_ror:8
     x[f] += dpp_move<0x124>(x[f]);                           // row_ror:4
   }
@@ -209,9 +209,11 @@ constexpr int cache8_scores_lds(int H, int ks, int w_bytes) {
 }
 
 // MODE 0: A_n = A_{n-1} + A_delta, 1: FFN(A_{n-1}) + A_delta, 2: FFN([A_{n-1}; A_delta]).  KS: pieces of 32 features of a K_LR row.
-// grid (ceil(Lk / 64), B), block 256: a page of a sequence, all heads.  The waves take the key/value heads in turn (A_delta to the LDS), then 16
-// tokens each through the FFN.  float32 A_n to `s` for k_cache8_pv.
-template <int HBI, int FS, int HBO, int ACT, int MODE, int KS>
+// grid (ceil(Lk / 64), B), block 256: a page of a sequence, all heads.  The waves take tiles of four heads in turn (A_delta to the LDS), then
+// 16 tokens each through the FFN.  float32 A_n to `s` for k_cache8_pv.
+// KVT: key/value heads that the four heads of a tile can have, 1 (groups of whole tiles) or 4; their products go into one accumulator, so that what
+// follows on the vector ALU (16 sums over the pieces) is done once per tile.
+template <int HBI, int FS, int HBO, int ACT, int MODE, int KS, int KVT>
 __global__ __launch_bounds__(256) void k_cache8_scores_mfma(Cache8ScoresArgs a) {
   typedef MfmaFfn<HBI, FS, HBO, ACT> Ffn;
   constexpr int KX = MODE == 0 ? 1 : Ffn::KS;
@@ -231,7 +233,30 @@ __global__ __launch_bounds__(256) void k_cache8_scores_mfma(Cache8ScoresArgs a) 
   if (page < 0) return;
   const int n = lane & 15, g = lane >> 4;
   const int pj = 16 * wv + n, j = col * PG_TOK + pj;         // this lane's token in the FFN
-  const int group = H / c.Hkv, GT = (group + 3) / 4, units = c.Hkv * GT;
+  const int group = H / c.Hkv, tiles = (H + 3) / 4;
+  const int hn = n & 3, pc = n >> 2;
+  // keys: the tiles of this wave, UN of them in flight
+  constexpr int UN = KVT == 1 ? 4 : KS == 1 ? 2 : 1;
+  const int np = c.w8 / 8;
+  struct Tile {
+    c8_u32x4 k[KVT][KS][2];
+    float scale;                                             // of this lane's head
+  };
+  Tile in[UN];
+  auto load_k = [&](int tile, Tile& t) {
+    const int first = min(4 * tile, H - 1), kv0 = first / group, kv1 = min(4 * tile + 3, H - 1) / group;
+    t.scale = c.k_scale[(size_t)page * c.Hkv + min(4 * tile + hn, H - 1) / group];
+#pragma unroll
+    for (int v = 0; v < KVT; ++v) {
+      const unsigned char* kb = c.k_block(page, min(kv0 + v, kv1));
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) t.k[v][s][u] = c8_stream(kb + (min(4 * s + g, np - 1) * PG_TOK + page_token(n, u)) * 8);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < UN; ++i) load_k(wv + 4 * i, in[i]);
   // A_{n-1} of this lane's token: what the FFN takes (clamped; past the heads and the end it is zeroed below)
   f16x8 x[1][KX];
   if (MODE != 0)
@@ -240,19 +265,6 @@ __global__ __launch_bounds__(256) void k_cache8_scores_mfma(Cache8ScoresArgs a) 
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         x[0][ks][e] = a.prev[((size_t)b * H + min(32 * ks + 8 * g + e, H - 1)) * a.Lk + min(j, len - 1)];
-  // keys: units of four heads of a key/value head, UN of them in flight
-  constexpr int UN = 4;
-  const int np = c.w8 / 8;
-  c8_u32x4 kreg[UN][KS][2];
-  auto load_k = [&](int unit, c8_u32x4 (&k)[KS][2]) {
-    const unsigned char* kb = c.k_block(page, min(unit, units - 1) / GT);
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) k[s][u] = c8_stream(kb + (min(4 * s + g, np - 1) * PG_TOK + page_token(n, u)) * 8);
-  };
-#pragma unroll
-  for (int i = 0; i < UN; ++i) load_k(wv + 4 * i, kreg[i]);
   auto src = [&](int h) { return a.q + ((size_t)b * H + h) * c.w; };
   if (a.fmt) stage_queries<1, 32 * KS>(H, c.w, q_s, e_s, tid, 256, src);
   else stage_queries<0, 32 * KS>(H, c.w, q_s, e_s, tid, 256, src);
@@ -261,36 +273,42 @@ __global__ __launch_bounds__(256) void k_cache8_scores_mfma(Cache8ScoresArgs a) 
     else Ffn::stage(a.w1, a.w2, Din, a.F, w_s, tid, 256, 0, H, H);
   }
   __syncthreads();
-  const int hn = n & 3, pc = n >> 2;
-  auto delta = [&](auto fmt, int unit, const c8_u32x4 (&k)[KS][2]) __attribute__((always_inline)) {
+  auto delta = [&](auto fmt, int tile, const Tile& t) __attribute__((always_inline)) {
     constexpr int FMT = decltype(fmt)::value;
-    const int kv = unit / GT, ht = 4 * (unit % GT) + hn, h = kv * group + min(ht, group - 1);
-    const bool live = ht < group && pc < 3;
+    typedef mfma8<FMT> M;
+    const int h = min(4 * tile + hn, H - 1), mine = h / group, kv0 = 4 * tile / group;
     unsigned long long qc[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       qc[s] = *(const unsigned long long*)(q_s + (h * 3 + min(pc, 2)) * (32 * KS) + 32 * s + 8 * g);
-      if (!live) qc[s] = 0;
+      if (pc == 3) qc[s] = 0;
     }
-    const float weight = mfma8<FMT>::query_weight(pc, e_s[h]) * (c.k_scale[(size_t)page * c.Hkv + kv] * a.scale);
+    typename M::acc acc[2][2] = {{M::zero(), M::zero()}, {M::zero(), M::zero()}};
+#pragma unroll
+    for (int v = 0; v < KVT; ++v) {
+      unsigned long long qv[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qv[s] = KVT == 1 || mine == kv0 + v ? qc[s] : 0;
+      page_products<FMT, KS>(t.k[v], qv, acc);
+    }
     float xs[16];
-    page_scores<FMT, KS>(k, qc, weight, xs);
-    if (ht < group) {                                        // lane (head, quarter, g): four of its sixteen tokens
+    page_sums<FMT>(acc, M::query_weight(pc, e_s[h]) * (t.scale * a.scale), xs);
+    if (4 * tile + hn < H) {                                 // lane (head, quarter, g): four of its sixteen tokens
       f32x4 y;
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] = pc == 0 ? xs[i] : pc == 1 ? xs[4 + i] : pc == 2 ? xs[8 + i] : xs[12 + i];
       *(f32x4*)(a_s + h * C8_SROW + 16 * g + 4 * pc) = y;
     }
   };
-  for (int u0 = wv; u0 < units; u0 += 4 * UN) {
+  for (int t0 = wv; t0 < tiles; t0 += 4 * UN) {
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
-      const int unit = u0 + 4 * i;
-      if (unit < units) {
-        if (a.fmt) delta(std::integral_constant<int, 1>{}, unit, kreg[i]);
-        else delta(std::integral_constant<int, 0>{}, unit, kreg[i]);
+      const int tile = t0 + 4 * i;
+      if (tile < tiles) {
+        if (a.fmt) delta(std::integral_constant<int, 1>{}, tile, in[i]);
+        else delta(std::integral_constant<int, 0>{}, tile, in[i]);
       }
-      if (u0 + 4 * UN < units) load_k(unit + 4 * UN, kreg[i]);
+      if (t0 + 4 * UN < tiles) load_k(tile + 4 * UN, in[i]);
     }
   }
   __syncthreads();
@@ -353,7 +371,7 @@ struct Cache8PvArgs {
 // 8 or 16 KB of a step.
 // GT: tiles of four query heads, GH: heads of a tile that are there (1: one query head per key/value head).
 template <int FMT, int DK, int MODE, int GT, int GH, int NW>
-__global__ __launch_bounds__(64 * NW) void k_cache8_pv(Cache8PvArgs a) {
+__global__ __launch_bounds__(64 * NW, NW == 4 && GT == 1 && GH == 1 && MODE < 2 ? (MODE == 1 ? 4 : 3) : 1) void k_cache8_pv(Cache8PvArgs a) {
   typedef mfma8<FMT> M;
   constexpr int KS = DK / 32, NT = DK / 16;
   constexpr float LOG2E = 1.4426950408889634f;
@@ -456,7 +474,9 @@ __global__ __launch_bounds__(64 * NW) void k_cache8_pv(Cache8PvArgs a) {
 #pragma unroll
     for (int t = 0; t < GT; ++t) {
       if constexpr (MODE == 0) {
-        page_scores<FMT, KS>(kreg, qc[t], qw[t] * k_scale, x[t]);
+        typename M::acc acc[2][2] = {{M::zero(), M::zero()}, {M::zero(), M::zero()}};
+        page_products<FMT, KS>(kreg, qc[t], acc);
+        page_sums<FMT>(acc, qw[t] * k_scale, x[t]);
       } else {
 #pragma unroll
         for (int f = 0; f < 16; ++f) x[t][f] = MODE == 1 ? sreg[t][f] : (float)hreg[t][f];

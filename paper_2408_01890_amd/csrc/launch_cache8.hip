@@ -6,10 +6,10 @@
 namespace lisa {
 
 namespace {
-template <int HBI, int FS, int HBO, int ACT, int MODE, int KS>
+template <int HBI, int FS, int HBO, int ACT, int MODE, int KS, int KVT>
 int launch_scores_t(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
   const int lds = cache8_scores_lds(d->H, KS, MODE == 0 ? 0 : MfmaFfn<HBI, FS, HBO, ACT>::kStageBytes);
-  auto kern = k_cache8_scores_mfma<HBI, FS, HBO, ACT, MODE, KS>;
+  auto kern = k_cache8_scores_mfma<HBI, FS, HBO, ACT, MODE, KS, KVT>;
   if (lds > 64 * 1024) {
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return hip_fail(e);
@@ -20,7 +20,8 @@ int launch_scores_t(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t s
 }
 template <int HBI, int FS, int HBO, int ACT, int MODE>
 int launch_scores_ks(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
-  return a.c.w <= 32 ? launch_scores_t<HBI, FS, HBO, ACT, MODE, 1>(d, a, st) : launch_scores_t<HBI, FS, HBO, ACT, MODE, 2>(d, a, st);
+  if (a.c.w > 32) return launch_scores_t<HBI, FS, HBO, ACT, MODE, 2, 4>(d, a, st);
+  return d->H / d->Hkv % 4 == 0 ? launch_scores_t<HBI, FS, HBO, ACT, MODE, 1, 1>(d, a, st) : launch_scores_t<HBI, FS, HBO, ACT, MODE, 1, 4>(d, a, st);
 }
 template <int HB, int ACT>
 int launch_add_fs(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {

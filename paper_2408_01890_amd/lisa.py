@@ -180,7 +180,7 @@ def _lib():
         h.lisa_pages_free.restype = C.c_int
         h.lisa_pages_compact.argtypes = [pp, vp, vp, sz, vp]
         h.lisa_pages_compact.restype = C.c_int
-        h.lisa_pages_copy.argtypes = [cp, C.c_int32, vp, C.c_int32, vp]
+        h.lisa_pages_copy.argtypes = [vp, C.c_int32, vp, C.c_int32, vp]   # (records on end)
         h.lisa_pages_copy.restype = C.c_int
         h.lisa_profile_collect.argtypes = [C.POINTER(StageTime), C.c_int]
         h.lisa_profile_collect.restype = C.c_int
@@ -770,11 +770,11 @@ PAGE_TOKENS = 64
 _FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
 
 
-def _on(device, **tensors):
+def _on(device, *tensors):
     """Raises ValueError unless the tensors that are given lie on `device` and that is the current one (the streams are its)."""
-    for name, t in tensors.items():
+    for t in tensors:
         if t is not None and t.device != device:
-            raise ValueError(f"{name}: on {t.device}, the cache on {device}")
+            raise ValueError(f"a tensor of shape {tuple(t.shape)} is on {t.device}, the cache on {device}")
     if device.index != torch._C._cuda_getDevice():
         raise ValueError(f"the cache is on {device}, which is not the current device")
 
@@ -782,7 +782,7 @@ def _on(device, **tensors):
 class Pages:
     """Which pages of the 8-bit caches the sequences of a server have (lisa_pages in include/lisa.h): `table`
     [n_seqs, max_pages], `lens` [n_seqs] and `refs` [n_pages], int32 device tensors that the caller owns and the lisa_pages_*
-    calls change in place.  All layers' caches share one."""
+    calls change in place (with scratch of the state's own: calls on one state follow each other).  All layers' caches share one."""
 
     def __init__(self, table, lens, refs):
         if table.dim() != 2 or table.numel() == 0 or refs.dim() != 1 or refs.numel() == 0:
@@ -798,6 +798,7 @@ class Pages:
         self._need = int(_lib().lisa_pages_workspace_bytes(self._ref))
         if self._need == 0:
             raise LisaError(-3, "Pages")
+        self._ws = torch.empty(self._need, dtype=torch.uint8, device=self.device)
 
     @classmethod
     def empty(cls, n_pages, n_seqs, max_pages, device="cuda"):
@@ -830,6 +831,7 @@ class Cache8:
                                 _ptr(k_scale, "k_scale", (P, Hkv), torch.float32), _ptr(v, "v"),
                                 _ptr(v_scale, "v_scale", (P, Hkv), torch.float32), pages._desc.table, pages._desc.lens)
         self._ref = C.byref(self._desc)
+        self._bytes = bytes(self._desc)
 
     @classmethod
     def empty(cls, pages, Hkv, width, d_k, format=torch.int8):
@@ -852,7 +854,7 @@ def lisa_cache8_append(cache, k_new, v_new, *, counts=None):
     B, _, L, _ = v_new.shape
     dt = v_new.dtype
     _sequences(cache, B)
-    _on(cache.device, k_new=k_new, v_new=v_new, counts=counts)
+    _on(cache.device, k_new, v_new, counts)
     if cache.width and k_new is None:
         raise ValueError("k_new: the cache has keys")
     desc, _ = _plan(None, dt, B, cache.Hkv, cache.Hkv, L, L, cache.d_k, cache.width, 0, MIX_ADD, ACT_RELU, 0.0, 0.0, 0)
@@ -884,8 +886,7 @@ def lisa_attn_decode8(q_lr, cache, score_row_prev, w1, w2, *, mix=MIX_ADD, act=A
     odt, of32 = _out_dtype(dt, out.dtype if out is not None else out_dtype)
     dk = cache.d_k
     _sequences(cache, B)
-    _on(cache.device, q_lr=q_lr, score_row_prev=score_row_prev, w1=w1, w2=w2, out=out, score_row_out=score_row_out,
-        workspace=workspace)
+    _on(cache.device, q_lr, score_row_prev, w1, w2, out, score_row_out, workspace)
     desc, need = _plan(WS_DECODE8, dt, B, H, cache.Hkv, 1, Lk, dk, r, F, mix, act, delta_scale, 0.0, 0, int(write_scores), 0, 0,
                        of32)
     if out is None:
@@ -913,7 +914,7 @@ def std_attn_decode8(q, cache, Lk, *, want_scores=True, std_scale=0.0, score_row
     dt = q.dtype
     odt, of32 = _out_dtype(dt, out.dtype if out is not None else out_dtype)
     _sequences(cache, B)
-    _on(cache.device, q=q, out=out, score_row_out=score_row_out, workspace=workspace)
+    _on(cache.device, q, out, score_row_out, workspace)
     desc, need = _plan(WS_STD_DECODE8, dt, B, H, cache.Hkv, 1, Lk, dk, 0, 0, MIX_ADD, ACT_RELU, 0.0, std_scale, 0, 0, 0, 0, of32)
     sdt = score_dtype(dt)
     if want_scores and score_row_out is None:
@@ -930,25 +931,24 @@ def std_attn_decode8(q, cache, Lk, *, want_scores=True, std_scale=0.0, score_row
     return (score_row_out if want_scores else None), out
 
 
-def _pages_call(name, pages, workspace, *args, **tensors):
-    _on(pages.device, workspace=workspace, **tensors)
-    workspace, wp, wb = _workspace(pages._need, pages.table, workspace)
-    rc = getattr(_lib(), name)(pages._ref, *args, wp, wb, _stream())
+def _pages_call(name, pages, *args):
+    rc = getattr(_lib(), name)(pages._ref, *args, pages._ws.data_ptr(), pages._need, _stream())
     if rc:
         raise LisaError(rc, name)
 
 
-def lisa_pages_grow(pages, add, *, done=None, workspace=None):
+def lisa_pages_grow(pages, add, *, done=None):
     """Gives sequence s add[s] (int32 [n_seqs]) more tokens and the pages they need.  Returns done [n_seqs] int32: 0 where a
     sequence is as it was, for lack of room."""
     if done is None:
         done = torch.empty(pages.n_seqs, dtype=torch.int32, device=pages.device)
-    _pages_call("lisa_pages_grow", pages, workspace, _ptr(add, "add", (pages.n_seqs,), torch.int32),
-                _ptr(done, "done", (pages.n_seqs,), torch.int32), add=add, done=done)
+    _on(pages.device, add, done)
+    _pages_call("lisa_pages_grow", pages, _ptr(add, "add", (pages.n_seqs,), torch.int32),
+                _ptr(done, "done", (pages.n_seqs,), torch.int32))
     return done
 
 
-def lisa_pages_fork(pages, src, dst, *, done=None, copies=None, workspace=None):
+def lisa_pages_fork(pages, src, dst, *, done=None, copies=None):
     """Makes the empty sequences dst (int32 [n]) what the sequences src are.  Returns (done [n], copies [n, 2]): the pages that
     lisa_pages_copy has to copy in every layer before the next append."""
     n = src.shape[0]
@@ -956,29 +956,29 @@ def lisa_pages_fork(pages, src, dst, *, done=None, copies=None, workspace=None):
         done = torch.empty(n, dtype=torch.int32, device=pages.device)
     if copies is None:
         copies = torch.empty((n, 2), dtype=torch.int32, device=pages.device)
-    _pages_call("lisa_pages_fork", pages, workspace, _ptr(src, "src", (n,), torch.int32), _ptr(dst, "dst", (n,), torch.int32), n,
-                _ptr(done, "done", (n,), torch.int32), _ptr(copies, "copies", (n, 2), torch.int32), src=src, dst=dst, done=done,
-                copies=copies)
+    _on(pages.device, src, dst, done, copies)
+    _pages_call("lisa_pages_fork", pages, _ptr(src, "src", (n,), torch.int32), _ptr(dst, "dst", (n,), torch.int32), n,
+                _ptr(done, "done", (n,), torch.int32), _ptr(copies, "copies", (n, 2), torch.int32))
     return done, copies
 
 
-def lisa_pages_free(pages, seqs, *, done=None, workspace=None):
+def lisa_pages_free(pages, seqs, *, done=None):
     """Empties the sequences seqs (int32 [n]).  Returns done [n] int32."""
     n = seqs.shape[0]
     if done is None:
         done = torch.empty(n, dtype=torch.int32, device=pages.device)
-    _pages_call("lisa_pages_free", pages, workspace, _ptr(seqs, "seqs", (n,), torch.int32), n,
-                _ptr(done, "done", (n,), torch.int32), seqs=seqs, done=done)
+    _on(pages.device, seqs, done)
+    _pages_call("lisa_pages_free", pages, _ptr(seqs, "seqs", (n,), torch.int32), n, _ptr(done, "done", (n,), torch.int32))
     return done
 
 
-def lisa_pages_compact(pages, *, copies=None, workspace=None):
+def lisa_pages_compact(pages, *, copies=None):
     """Moves the used pages to the front of the pool in the page state.  Returns copies [n_pages // 2, 2], which lisa_pages_copy has
     to copy in every layer before anything else uses the caches."""
     if copies is None:
         copies = torch.empty((pages.n_pages // 2, 2), dtype=torch.int32, device=pages.device)
-    _pages_call("lisa_pages_compact", pages, workspace, _ptr(copies, "copies", (pages.n_pages // 2, 2), torch.int32),
-                copies=copies)
+    _on(pages.device, copies)
+    _pages_call("lisa_pages_compact", pages, _ptr(copies, "copies", (pages.n_pages // 2, 2), torch.int32))
     return copies
 
 
@@ -988,9 +988,10 @@ def lisa_pages_copy(caches, copies):
     if not caches or copies.shape[0] == 0:
         return
     for c in caches:
-        _on(c.device, copies=copies)
-    arr = (Cache8Desc * len(caches))(*[c._desc for c in caches])
-    rc = _lib().lisa_pages_copy(arr, len(caches), _ptr(copies, "copies", (copies.shape[0], 2), torch.int32), copies.shape[0],
-                                _stream())
+        if c.device != copies.device:
+            raise ValueError(f"copies on {copies.device}, a cache on {c.device}")
+    _on(copies.device)
+    rc = _lib().lisa_pages_copy(b"".join([c._bytes for c in caches]), len(caches),
+                                _ptr(copies, "copies", (copies.shape[0], 2), torch.int32), copies.shape[0], _stream())
     if rc:
         raise LisaError(rc, "lisa_pages_copy")
