@@ -81,37 +81,54 @@ __device__ __forceinline__ void query_pieces(const float (&x)[4], int e, unsigne
   }
 }
 // The pieces of H rows of n <= W elements in the LDS, codes [h][piece][W], exps [h], by all threads of the workgroup
-// (W / 4 lanes, at most 64, per row).  src(h): the row, null: zeros.
-template <int FMT, int W, class Src>
-__device__ __forceinline__ void stage_queries(int H, int n, unsigned char* codes, int* exps, int tid, int nthreads, Src&& src) {
-  constexpr int LPR = W / 4;                                 // lanes per row (a power of two)
-  static_assert(LPR <= 64 && (LPR & (LPR - 1)) == 0, "lanes per row");
-  for (int e0 = 0; e0 < H * LPR; e0 += nthreads) {           // (nthreads is a multiple of LPR: whole rows)
-    const int h = (e0 + tid) / LPR, l = tid % LPR;
-    const bf16_t* q = h < H ? src(h) : nullptr;
-    float x[4], m = 0.f;
-    int bad = 0;
+// (W / 4 lanes, at most 64, per row).  src(h): the row.  load() issues the loads of the first rows; what is loaded between it and
+// store() does not have to arrive for them.
+template <int FMT, int W>
+__device__ __forceinline__ void store_query(const unsigned short (&raw)[4], int h, int l, int H, int n, unsigned char* codes, int* exps) {
+  constexpr int LPR = W / 4;
+  float x[4], m = 0.f;
+  int bad = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = q && 4 * l + i < n ? elem<bf16_t>::load(q + 4 * l + i) : 0.f;
-      bad |= !(fabsf(x[i]) < INFINITY);
-      m = fmaxf(m, fabsf(x[i]));
-    }
+  for (int i = 0; i < 4; ++i) {
+    x[i] = 4 * l + i < n ? bf16_bits_to_f32(raw[i]) : 0.f;
+    bad |= !(fabsf(x[i]) < INFINITY);
+    m = fmaxf(m, fabsf(x[i]));
+  }
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) {
-      m = fmaxf(m, __shfl_xor(m, o, 64));
-      bad |= __shfl_xor(bad, o, 64);
-    }
-    const int e = m > 0.f && !bad ? __builtin_amdgcn_frexp_expf(m) - 1 : 0;
-    unsigned w[3];
-    query_pieces<FMT>(x, e, w);
-    if (h < H) {
+  for (int o = LPR / 2; o > 0; o >>= 1) {
+    m = fmaxf(m, __shfl_xor(m, o, 64));
+    bad |= __shfl_xor(bad, o, 64);
+  }
+  const int e = m > 0.f && !bad ? __builtin_amdgcn_frexp_expf(m) - 1 : 0;
+  unsigned w[3];
+  query_pieces<FMT>(x, e, w);
+  if (h < H) {
 #pragma unroll
-      for (int p = 0; p < 3; ++p) *(unsigned*)(codes + (h * 3 + p) * W + 4 * l) = w[p];
-      if (l == 0) exps[h] = bad ? C8_NO_QUERY : e;
-    }
+    for (int p = 0; p < 3; ++p) *(unsigned*)(codes + (h * 3 + p) * W + 4 * l) = w[p];
+    if (l == 0) exps[h] = bad ? C8_NO_QUERY : e;
   }
 }
+template <int W>
+struct QueryStage {
+  static constexpr int LPR = W / 4;                          // lanes per row (a power of two)
+  static_assert(LPR <= 64 && (LPR & (LPR - 1)) == 0, "lanes per row");
+  unsigned short raw[4];
+  template <class Src>
+  __device__ __forceinline__ void load(int e0, int H, int n, int tid, Src&& src) {
+    const bf16_t* q = src(min((e0 + tid) / LPR, H - 1));
+    const int l = tid % LPR;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = q[min(4 * l + i, n - 1)].bits;
+  }
+  template <class Src>
+  __device__ __forceinline__ void store(bool e4m3, int H, int n, unsigned char* codes, int* exps, int tid, int nthreads, Src&& src) {
+    for (int e0 = 0; e0 < H * LPR; e0 += nthreads) {         // (nthreads is a multiple of LPR: whole rows)
+      if (e0) load(e0, H, n, tid, src);
+      if (e4m3) store_query<1, W>(raw, (e0 + tid) / LPR, tid % LPR, H, n, codes, exps);
+      else store_query<0, W>(raw, (e0 + tid) / LPR, tid % LPR, H, n, codes, exps);
+    }
+  }
+};
 
 // Scores of a page against the four heads of a tile: x[f] = score of token 16 g + f, head n % 4.
 // kreg[s][u]: 16 bytes of a lane, tokens T and T + 1 (T = 16 (n / 4) + 8 u + 2 (n % 4)), features 32 s + 8 g .. + 7.  page_products may be
@@ -134,6 +151,17 @@ __device__ __forceinline__ void page_sums(const typename mfma8<FMT>::acc (&acc)[
     x[f] = (float)acc[f >> 3][f & 1][(f & 7) >> 1] * weight;
     x[f] += dpp_move<0x128>(x[f]);                           // row_ror:8
     x[f] += dpp_move<0x124>(x[f]);                           // row_ror:4
+  }
+}
+// The four of sixteen values that quarter `pc` of the lanes keeps.  (The values are pinned: else the choice becomes branches around what
+// they are made of.)
+__device__ __forceinline__ void quarter(float (&x)[16], int pc, float (&y)[4]) {
+#pragma unroll
+  for (int f = 0; f < 16; ++f) asm volatile("" : "+v"(x[f]));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = pc & 1 ? x[4 + i] : x[i], hi = pc & 1 ? x[12 + i] : x[8 + i];
+    y[i] = pc & 2 ? hi : lo;
   }
 }
 __device__ __forceinline__ int page_token(int n, int u) { return 16 * (n >> 2) + 8 * u + 2 * (n & 3); }
@@ -170,7 +198,7 @@ __device__ __forceinline__ void prob_pieces(const float (&p)[16], int pc, unsign
         y[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8((int)c[k], 2)) * 16.f;
         y[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8((int)c[k], 3)) * 16.f;
       }
-      w[q] = pc == 0 ? c[0] : pc == 1 ? c[1] : pc == 2 ? c[2] : 0u;
+      w[q] = pc & 2 ? (pc & 1 ? 0u : c[2]) : pc & 1 ? c[1] : c[0];
     }
   }
   op[0] = w[0] | (unsigned long long)w[1] << 32;
@@ -195,56 +223,142 @@ struct Cache8ScoresArgs {
   Cache8View c;
   const bf16_t* q;            // [B,H,w]
   const half_t* prev;         // [B,H,Lk]
-  const bf16_t* w1;           // [Din,F], [F,H]; or
-  const bf16_t* w2;
-  const unsigned short* img;  // the same in operand order (ffn_operand_piece<false>), if not null
+  const bf16_t* w1;           // [Din,F]
+  const bf16_t* w2;           // [F,H]; null: a single layer (w1 is [Din,H], F = 2 H)
   half_t* row;                // [B,H,Lk] or null
-  float* s;                   // [B,H,Lp]
+  float* s;                   // A_n, [B][pages][H][64]
   int H, Lk, Lp, F, fmt;
+  int n_pages;                // pages per workgroup, at most 64
   float scale;
 };
 constexpr int C8_SROW = PG_TOK + 4;                          // floats per head of the a_delta tile
-constexpr int cache8_scores_lds(int H, int ks, int w_bytes) {
-  return (H * C8_SROW + (H + 3) / 4 * 4) * 4 + H * 3 * 32 * ks + w_bytes;
+constexpr int cache8_scores_lds(int H, int ks, int w_bytes) {   // (a row more per tile: what lies past the heads)
+  return (2 * (H + 1) * C8_SROW + (H + 3) / 4 * 4) * 4 + H * 3 * 32 * ks + w_bytes;
 }
 
+// The image of MfmaFfn::stage() by 256 threads.  Rows of even length: a thread takes eight rows of two columns, which are two 16-byte pieces of
+// the image; load() issues all loads (ahead of the first page's), store() puts them in place.  (64 -> 256 -> 32, 8 x 2500 tokens: 31 us for the launch with
+// 16-byte loads along the rows, whose elements go to LDS banks that collide; 19 with a launch in front that makes the image.)  w2 null:
+// y = w1^T x as the ReLU network [w1, -w1], [I; -I].
+template <int KS, int FS, int HBO>
+struct FfnStage {
+  static constexpr int T1 = KS * 4 * 16 * FS, T2 = FS * 4 * 8 * HBO;   // (k-step, g, column pair)
+  static constexpr int N1 = (T1 + 255) / 256, N2 = (T2 + 255) / 256;
+  unsigned x1[N1][8], x2[N2][8];
+  static __device__ __forceinline__ bool pairs(const Cache8ScoresArgs& a) { return a.w2 && a.F % 2 == 0 && a.H % 2 == 0; }
+  __device__ __forceinline__ void load(const Cache8ScoresArgs& a, int Din, int tid) {
+    if (!pairs(a)) return;
+#pragma unroll
+    for (int i = 0; i < N1; ++i) {
+      const int e = min(tid + 256 * i, T1 - 1), f = 2 * (e % (16 * FS)), r = e / (16 * FS) * 8;   // rows r .. r + 7
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x1[i][k] = *(const unsigned*)(a.w1 + (unsigned)min(r + k, Din - 1) * a.F + min(f, a.F - 2));
+    }
+#pragma unroll
+    for (int i = 0; i < N2; ++i) {
+      const int e = min(tid + 256 * i, T2 - 1), h = 2 * (e % (8 * HBO)), o = e / (8 * HBO), r = 32 * (o >> 2) + 4 * (o & 3);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x2[i][k] = *(const unsigned*)(a.w2 + (unsigned)min(r + 16 * (k >> 2) + (k & 3), a.F - 1) * a.H + min(h, a.H - 2));
+    }
+  }
+  __device__ __forceinline__ static unsigned short* at1(unsigned short* lds, int ch, int f) {
+    return lds + (((f >> 4) * KS + (ch >> 5)) * 64 + (ch >> 3 & 3) * 16 + (f & 15)) * 8 + (ch & 7);
+  }
+  __device__ __forceinline__ static unsigned short* at2(unsigned short* lds, int f, int h) {
+    const int r = f & 31;
+    return lds + 2 * FS * KS * 512 + (((h >> 4) * FS + (f >> 5)) * 64 + (r >> 2 & 3) * 16 + (h & 15)) * 8 + 4 * (r >> 4) + (r & 3);
+  }
+  // the low (high) halves of eight pairs, as halves, zero where `in` says so
+  template <class In>
+  __device__ __forceinline__ static u16x8 piece(const unsigned (&x)[8], int high, In&& in) {
+    u16x8 v;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = in(k) ? half_bits(high ? __uint_as_float(x[k] & 0xffff0000u) : bf16_bits_to_f32(x[k] & 0xffffu)) : (unsigned short)0;
+    return v;
+  }
+  __device__ __forceinline__ void store(const Cache8ScoresArgs& a, int Din, unsigned short* lds, int tid) {
+    if (pairs(a)) {
+#pragma unroll
+      for (int i = 0; i < N1; ++i) {
+        const int e = tid + 256 * i, f = 2 * (e % (16 * FS)), r = e / (16 * FS) * 8;
+        if (e < T1)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) *(u16x8*)at1(lds, r, f + c) = piece(x1[i], c, [&](int k) { return r + k < Din && f < a.F; });
+      }
+#pragma unroll
+      for (int i = 0; i < N2; ++i) {
+        const int e = tid + 256 * i, h = 2 * (e % (8 * HBO)), o = e / (8 * HBO), r = 32 * (o >> 2) + 4 * (o & 3);
+        if (e < T2)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) *(u16x8*)at2(lds, r, h + c) = piece(x2[i], c, [&](int k) { return r + 16 * (k >> 2) + (k & 3) < a.F && h < a.H; });
+      }
+      return;
+    }
+    const int H = a.H, cols = a.w2 ? a.F : H;
+#pragma unroll 4
+    for (int e = tid; e < 32 * KS * 32 * FS; e += 256) {
+      const int ch = e / (32 * FS), f = e % (32 * FS);
+      const unsigned v = a.w1[(size_t)min(ch, Din - 1) * cols + min(f < cols ? f : f - cols, cols - 1)].bits;
+      const float y = bf16_bits_to_f32(v);
+      *at1(lds, ch, f) = ch < Din && f < a.F ? half_bits(f < cols ? y : -y) : (unsigned short)0;
+    }
+#pragma unroll 4
+    for (int e = tid; e < 32 * FS * 16 * HBO; e += 256) {
+      const int f = e / (16 * HBO), h = e % (16 * HBO);
+      float y = f == h ? 1.f : f == H + h ? -1.f : 0.f;
+      if (a.w2) y = bf16_bits_to_f32(a.w2[(size_t)min(f, a.F - 1) * H + min(h, H - 1)].bits);
+      *at2(lds, f, h) = f < a.F && h < H ? half_bits(y) : (unsigned short)0;
+    }
+  }
+};
+
+#ifndef C8_SCORES_WAVES
+#define C8_SCORES_WAVES(MODE, KVT, KS) 2
+#endif
 // MODE 0: A_n = A_{n-1} + A_delta, 1: FFN(A_{n-1}) + A_delta, 2: FFN([A_{n-1}; A_delta]).  KS: pieces of 32 features of a K_LR row.
-// grid (ceil(Lk / 64), B), block 256: a page of a sequence, all heads.  The waves take tiles of four heads in turn (A_delta to the LDS), then
-// 16 tokens each through the FFN.  float32 A_n to `s` for k_cache8_pv.
+// grid (ceil(pages / n_pages), B), block 256: n_pages pages of a sequence, all heads.  Per page the waves take tiles of four heads in turn
+// (A_delta to the LDS), then 16 tokens each through the FFN; the next page's keys and A_{n-1} are loaded where this one's have been used, and one
+// barrier a page (two A_delta tiles) lets the waves run apart.  float32 A_n to `s` for k_cache8_pv.
 // KVT: key/value heads that the four heads of a tile can have, 1 (groups of whole tiles) or 4; their products go into one accumulator, so that what
 // follows on the vector ALU (16 sums over the pieces) is done once per tile.
 template <int HBI, int FS, int HBO, int ACT, int MODE, int KS, int KVT>
-__global__ __launch_bounds__(256) void k_cache8_scores_mfma(Cache8ScoresArgs a) {
+__global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_scores_mfma(Cache8ScoresArgs a) {
   typedef MfmaFfn<HBI, FS, HBO, ACT> Ffn;
   constexpr int KX = MODE == 0 ? 1 : Ffn::KS;
   extern __shared__ __align__(16) float c8_lds[];
   const Cache8View& c = a.c;
   const int H = a.H, Din = MODE == 2 ? 2 * H : H;
-  float* a_s = c8_lds;                                       // [H][C8_SROW]
-  int* e_s = (int*)(a_s + H * C8_SROW);                      // [H]
+  float* a_s = c8_lds;                                       // [2][H + 1][C8_SROW]
+  int* e_s = (int*)(a_s + 2 * (H + 1) * C8_SROW);            // [H]
   unsigned char* q_s = (unsigned char*)(e_s + (H + 3) / 4 * 4);   // [H][3][32 KS]
   unsigned short* w_s = (unsigned short*)(q_s + H * 3 * 32 * KS);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = blockIdx.x, b = blockIdx.y;
+  const int col0 = blockIdx.x * a.n_pages, b = blockIdx.y;
   const int len = min(c.lens[b], a.Lk);
-  if (col * PG_TOK >= len) return;
-  const int page = c.page_of(b, col);
-  if (page < 0) return;
+  const int my_col = col0 + lane;                            // lane i: the workgroup's page i
+  const int id = lane < a.n_pages && (long long)my_col * PG_TOK < len ? c.page_of(b, my_col) : -1;
+  unsigned long long todo = __ballot(id >= 0);
+  if (!todo) return;
   const int n = lane & 15, g = lane >> 4;
-  const int pj = 16 * wv + n, j = col * PG_TOK + pj;         // this lane's token in the FFN
+  const int pj = 16 * wv + n;                                // this lane's token in the FFN
   const int group = H / c.Hkv, tiles = (H + 3) / 4;
   const int hn = n & 3, pc = n >> 2;
   // keys: the tiles of this wave, UN of them in flight
-  constexpr int UN = KVT == 1 ? 4 : KS == 1 ? 2 : 1;
+  constexpr int UN = KVT == 4 || KS == 2 ? 1 : 2;            // (two tiles of four key/value heads do not fit the register file)
   const int np = c.w8 / 8;
+  const int rounds = (tiles + 4 * UN - 1) / (4 * UN);        // of UN tiles per wave and page (past the last tile: the last one again)
+  unsigned k_at[KS];                                         // this lane's place in a block of keys
+#pragma unroll
+  for (int s = 0; s < KS; ++s) k_at[s] = (min(4 * s + g, np - 1) * PG_TOK + page_token(n, 0)) * 8;
   struct Tile {
     c8_u32x4 k[KVT][KS][2];
     float scale;                                             // of this lane's head
   };
   Tile in[UN];
-  auto load_k = [&](int tile, Tile& t) {
-    const int first = min(4 * tile, H - 1), kv0 = first / group, kv1 = min(4 * tile + 3, H - 1) / group;
+  auto load_k = [&](int page, int tile, Tile& t) {
+    tile = min(tile, tiles - 1);
+    const int kv0 = 4 * tile / group, kv1 = min(4 * tile + 3, H - 1) / group;
     t.scale = c.k_scale[(size_t)page * c.Hkv + min(4 * tile + hn, H - 1) / group];
 #pragma unroll
     for (int v = 0; v < KVT; ++v) {
@@ -252,28 +366,42 @@ __global__ __launch_bounds__(256) void k_cache8_scores_mfma(Cache8ScoresArgs a) 
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) t.k[v][s][u] = c8_stream(kb + (min(4 * s + g, np - 1) * PG_TOK + page_token(n, u)) * 8);
+        for (int u = 0; u < 2; ++u) t.k[v][s][u] = c8_stream(kb + k_at[s] + u * 64);
     }
   };
+  // A_{n-1} of this lane's token: what the FFN takes (clamped; past the heads and the end it is zeroed where it is used).  One element per
+  // register: to pack them is to wait for them.
+  unsigned short xin[KX][8];
+  auto load_x = [&](int i) {
+    const unsigned short* xp = (const unsigned short*)a.prev + (size_t)b * H * a.Lk;   // (32-bit offsets: H Lk < 2^30)
+    const unsigned j = min((col0 + i) * PG_TOK + pj, len - 1);
+    if (MODE != 0)
 #pragma unroll
-  for (int i = 0; i < UN; ++i) load_k(wv + 4 * i, in[i]);
-  // A_{n-1} of this lane's token: what the FFN takes (clamped; past the heads and the end it is zeroed below)
-  f16x8 x[1][KX];
-  if (MODE != 0)
+      for (int ks = 0; ks < KX; ++ks)
 #pragma unroll
-    for (int ks = 0; ks < KX; ++ks)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        x[0][ks][e] = a.prev[((size_t)b * H + min(32 * ks + 8 * g + e, H - 1)) * a.Lk + min(j, len - 1)];
+        for (int e = 0; e < 8; ++e) xin[ks][e] = xp[(unsigned)min(32 * ks + 8 * g + e, H - 1) * (unsigned)a.Lk + j];
+  };
   auto src = [&](int h) { return a.q + ((size_t)b * H + h) * c.w; };
-  if (a.fmt) stage_queries<1, 32 * KS>(H, c.w, q_s, e_s, tid, 256, src);
-  else stage_queries<0, 32 * KS>(H, c.w, q_s, e_s, tid, 256, src);
-  if (MODE != 0) {
-    if (a.img) Ffn::stage(a.img, w_s, tid, 256);
-    else Ffn::stage(a.w1, a.w2, Din, a.F, w_s, tid, 256, 0, H, H);
+  QueryStage<32 * KS> qst;
+  qst.load(0, H, c.w, tid, src);
+  FfnStage<KX, FS, HBO> fst;
+  if (MODE != 0) fst.load(a, Din, tid);
+  if (MODE == 2) {                                           // (a wide network: its registers first)
+    __builtin_amdgcn_sched_barrier(0);
+    fst.store(a, Din, w_s, tid);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  __syncthreads();
-  auto delta = [&](auto fmt, int tile, const Tile& t) __attribute__((always_inline)) {
+  int at = __builtin_ctzll(todo), buf = 0;
+  {
+    const int page = __builtin_amdgcn_readlane(id, at);
+#pragma unroll
+    for (int i = 0; i < UN; ++i) load_k(page, wv + 4 * i, in[i]);
+    load_x(at);
+  }
+  qst.store(a.fmt, H, c.w, q_s, e_s, tid, 256, src);
+  if (MODE == 1) fst.store(a, Din, w_s, tid);
+  lds_barrier();
+  auto delta = [&](auto fmt, int tile, const Tile& t, float* to) __attribute__((always_inline)) {
     constexpr int FMT = decltype(fmt)::value;
     typedef mfma8<FMT> M;
     const int h = min(4 * tile + hn, H - 1), mine = h / group, kv0 = 4 * tile / group;
@@ -293,67 +421,110 @@ __global__ __launch_bounds__(256) void k_cache8_scores_mfma(Cache8ScoresArgs a) 
     }
     float xs[16];
     page_sums<FMT>(acc, M::query_weight(pc, e_s[h]) * (t.scale * a.scale), xs);
+    float y[4];
+    quarter(xs, pc, y);
     if (4 * tile + hn < H) {                                 // lane (head, quarter, g): four of its sixteen tokens
-      f32x4 y;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = pc == 0 ? xs[i] : pc == 1 ? xs[4 + i] : pc == 2 ? xs[8 + i] : xs[12 + i];
-      *(f32x4*)(a_s + h * C8_SROW + 16 * g + 4 * pc) = y;
+      *(f32x4*)(to + h * C8_SROW + 16 * g + 4 * pc) = f32x4{y[0], y[1], y[2], y[3]};
     }
   };
-  for (int t0 = wv; t0 < tiles; t0 += 4 * UN) {
+  auto step = [&](int next, auto more) __attribute__((always_inline)) {
+    constexpr bool MORE = decltype(more)::value;
+    const int page = __builtin_amdgcn_readlane(id, at), page_n = MORE ? __builtin_amdgcn_readlane(id, next) : 0;
+    float* to = a_s + buf * (H + 1) * C8_SROW;
+    auto tile_of = [&](int r, int i) { return wv + 4 * (r * UN + i); };
+    auto use = [&](int r, int i) __attribute__((always_inline)) {
+      if (tile_of(r, i) >= tiles) return;
+      if (a.fmt) delta(std::integral_constant<int, 1>{}, tile_of(r, i), in[i], to);
+      else delta(std::integral_constant<int, 0>{}, tile_of(r, i), in[i], to);
+    };
+    for (int r = 0; r + 1 < rounds; ++r)
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-      const int tile = t0 + 4 * i;
-      if (tile < tiles) {
-        if (a.fmt) delta(std::integral_constant<int, 1>{}, tile, in[i]);
-        else delta(std::integral_constant<int, 0>{}, tile, in[i]);
+      for (int i = 0; i < UN; ++i) {
+        use(r, i);
+        load_k(page, tile_of(r + 1, i), in[i]);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (t0 + 4 * UN < tiles) load_k(tile + 4 * UN, in[i]);
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {                           // (no branch around these loads: what comes after them waits for older ones only)
+      use(rounds - 1, i);
+      if (MORE) load_k(page_n, tile_of(0, i), in[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
-  __syncthreads();
-  if constexpr (MODE == 0) {
-    for (int e = tid; e < H * PG_TOK; e += 256) {
-      const int h = e >> 6, t = e & 63, jt = col * PG_TOK + t;
-      if (jt >= len) continue;
-      const size_t at = ((size_t)b * H + h) * a.Lk + jt;
-      const float y = (float)a.prev[at] + a_s[h * C8_SROW + t];
-      if (a.row) a.row[at] = f32_to_half_sat(y);
-      a.s[((size_t)b * H + h) * a.Lp + jt] = y;
+    lds_barrier();
+    // A_n of sixteen tokens of a wave's: lane -> head (16 of them at a time), four tokens
+    const int t_out = 16 * wv + 4 * (lane & 3), j_out = (col0 + at) * PG_TOK + t_out, h_out = lane >> 2;
+    float* sp = a.s + ((size_t)b * (a.Lp / PG_TOK) + col0 + at) * H * PG_TOK + t_out;
+    half_t* rp = a.row ? a.row + (size_t)b * H * a.Lk + j_out : nullptr;
+    auto emit = [&](int h, const f32x4& y) __attribute__((always_inline)) {
+      *(f32x4*)(sp + h * PG_TOK) = y;
+      if (!rp) return;
+      half_t* r = rp + (size_t)h * a.Lk;
+      typedef _Float16 f16x4_ __attribute__((ext_vector_type(4)));
+      const f16x4_ v = {f32_to_half_sat(y[0]), f32_to_half_sat(y[1]), f32_to_half_sat(y[2]), f32_to_half_sat(y[3])};
+      if (MORE || j_out + 4 <= len) {                        // (a page with another one behind it is full)
+        *(c8_u64_a2*)r = __builtin_bit_cast(unsigned long long, v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (j_out + i < len) r[i] = v[i];
+      }
+    };
+    if constexpr (MODE == 0) {
+      for (int h = h_out; h < H; h += 16) {
+        f32x4 y = *(const f32x4*)(to + h * C8_SROW + t_out);
+        const half_t* xp = a.prev + ((size_t)b * H + h) * a.Lk;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += (float)xp[min(j_out + i, len - 1)];
+        emit(h, y);
+      }
+    } else {
+      f16x8 x[1][KX];
+#pragma unroll
+      for (int ks = 0; ks < KX; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int ch = 32 * ks + 8 * g + e;
+          x[0][ks][e] = __builtin_bit_cast(half_t, xin[ks][e]);
+          if (MODE == 2 && ch >= H) x[0][ks][e] = ch < Din ? f32_to_half_sat(to[(ch - H) * C8_SROW + pj]) : (_Float16)0.f;
+          else if (ch >= Din) x[0][ks][e] = (_Float16)0.f;
+        }
+      if (MORE) load_x(next);
+      f32x4 y[1][HBO];
+      if (MODE == 2) Ffn::template apply_lds_lean<1>(w_s, x, y);
+      else Ffn::template apply_lds<1>(w_s, x, y);
+      // this wave's tokens of the tile become A_n (no other wave has business with them), and go out as rows
+      float d[HBO][4];
+#pragma unroll
+      for (int hb = 0; hb < HBO; ++hb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) d[hb][v] = MODE == 2 ? 0.f : to[min(16 * hb + 4 * g + v, H) * C8_SROW + pj];
+#pragma unroll
+      for (int hb = 0; hb < HBO; ++hb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          to[min(16 * hb + 4 * g + v, H) * C8_SROW + pj] = y[0][hb][v] + d[hb][v];
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int hb = 0; hb < HBO; ++hb)
+        if (16 * hb + h_out < H) emit(16 * hb + h_out, *(const f32x4*)(to + (16 * hb + h_out) * C8_SROW + t_out));
     }
-  } else {
-#pragma unroll
-    for (int ks = 0; ks < KX; ++ks)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int ch = 32 * ks + 8 * g + e;
-        if (MODE == 2 && ch >= H) x[0][ks][e] = ch < Din ? f32_to_half_sat(a_s[(ch - H) * C8_SROW + pj]) : (_Float16)0.f;
-        else if (ch >= Din) x[0][ks][e] = (_Float16)0.f;
-      }
-    f32x4 y[1][HBO];
-    if (MODE == 2) Ffn::template apply_lds_lean<1>(w_s, x, y);
-    else Ffn::template apply_lds<1>(w_s, x, y);
-    if (j >= len) return;
-    float* sp = a.s + (size_t)b * H * a.Lp + j;
-    half_t* rp = a.row + (size_t)b * H * a.Lk + j;
-#pragma unroll
-    for (int hb = 0; hb < HBO; ++hb)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int h = 16 * hb + 4 * g + v;
-        if (h >= H) continue;
-        const float an = y[0][hb][v] + (MODE == 2 ? 0.f : a_s[h * C8_SROW + pj]);
-        sp[(size_t)h * a.Lp] = an;
-        if (a.row) rp[(size_t)h * a.Lk] = f32_to_half_sat(an);
-      }
+    buf ^= 1;
+  };
+  todo &= todo - 1;
+  while (todo) {
+    const int next = __builtin_ctzll(todo);
+    todo &= todo - 1;
+    step(next, std::true_type{});
+    at = next;
   }
+  step(0, std::false_type{});
 }
 
 // ---- softmax and P V --------------------------------------------------------------------------------
 struct Cache8PvArgs {
   Cache8View c;
   const bf16_t* q;        // MODE 0: [B,H,DK]
-  const float* s;         // MODE 1: A_n [B,H,Lp]
+  const float* s;         // MODE 1: A_n [B][pages][H][64]
   const half_t* prev;     // MODE 2: A_n [B,H,Lk]
   half_t* row;            // MODE 0, 2: A_n out [B,H,Lk] or null
   void* out;              // [B,H,DK]
@@ -418,7 +589,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && GT == 1 && GH == 1 && MODE < 2 
     if constexpr (MODE == 1) {
 #pragma unroll
       for (int t = 0; t < GT; ++t) {
-        const float* sp = a.s + ((size_t)b * a.H + head0 + min(4 * t + hn, heads - 1)) * a.Lp + j;
+        const float* sp = a.s + (((size_t)b * (a.Lp / PG_TOK) + p_begin + wv + NW * i) * a.H + head0 + min(4 * t + hn, heads - 1)) * PG_TOK + 16 * g;
 #pragma unroll
         for (int q = 0; q < 4; ++q) *(f32x4*)&sreg[t][4 * q] = *(const f32x4*)(sp + 4 * q);
       }
@@ -432,6 +603,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && GT == 1 && GH == 1 && MODE < 2 
       }
     }
   };
+  QueryStage<DK> qst;
+  auto src = [&](int h) { return a.q + ((size_t)b * a.H + head0 + min(h, heads - 1)) * DK; };
+  if constexpr (MODE == 0) qst.load(0, GT * 4, DK, tid, src);
   int i = todo ? __builtin_ctzll(todo) : 0;
   if (todo) {
     load_k(i);
@@ -441,9 +615,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && GT == 1 && GH == 1 && MODE < 2 
   unsigned long long qc[MODE == 0 ? GT : 1][KS];
   float qw[MODE == 0 ? GT : 1];
   if constexpr (MODE == 0) {
-    stage_queries<FMT, DK>(GT * 4, DK, q_s, e_s, tid, 64 * NW,
-                           [&](int h) { return h < heads ? a.q + ((size_t)b * a.H + head0 + h) * DK : nullptr; });
-    __syncthreads();
+    qst.store(FMT == 1, GT * 4, DK, q_s, e_s, tid, 64 * NW, src);
+    lds_barrier();
 #pragma unroll
     for (int t = 0; t < GT; ++t) {
 #pragma unroll
@@ -489,10 +662,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && GT == 1 && GH == 1 && MODE < 2 
 #pragma unroll
     for (int t = 0; t < GT; ++t) {
       if (MODE != 1 && a.row && 4 * t + hn < heads) {        // lane (head, quarter, g): four of its sixteen tokens
+        float z[4];
+        quarter(x[t], pc, z);
         half_t y[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          y[e] = f32_to_half_sat(pc == 0 ? x[t][e] : pc == 1 ? x[t][4 + e] : pc == 2 ? x[t][8 + e] : x[t][12 + e]);
+        for (int e = 0; e < 4; ++e) y[e] = f32_to_half_sat(z[e]);
         const int tok = 16 * g + 4 * pc;
         half_t* rp = a.row + ((size_t)b * a.H + head0 + 4 * t + hn) * a.Lk + col * PG_TOK + tok;
         if (tok + 4 <= n_here) {

@@ -15,7 +15,8 @@ int launch_scores_t(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t s
     if (e != hipSuccess) return hip_fail(e);
   }
   StageScope prof("k_cache8_scores_mfma", st);
-  kern<<<dim3((d->Lk + PG_TOK - 1) / PG_TOK, d->B), 256, lds, st>>>(a);
+  const int pages = (d->Lk + PG_TOK - 1) / PG_TOK;
+  kern<<<dim3((pages + a.n_pages - 1) / a.n_pages, d->B), 256, lds, st>>>(a);
   return check_launch();
 }
 template <int HBI, int FS, int HBO, int ACT, int MODE>
@@ -97,7 +98,7 @@ template int launch_cache8_pv<LISA_PART - 4>(const lisa_desc*, int, int, const C
 
 namespace {
 
-// The module that the scores kernel runs: a single layer y = W^T x is the ReLU network [W, -W], [I; -I] (k_synth_relu_ffn).
+// The module that the scores kernel runs: a single layer y = W^T x is the ReLU network [W, -W], [I; -I] (stage_ffn).
 struct Module {
   int Din, F, act, mix;
 };
@@ -109,20 +110,6 @@ Module module_of(const lisa_desc* d) {
   m.act = d->act == LISA_ACT_SILU ? 1 : 0;
   return m;
 }
-FfnOperands operand_shape(const lisa_desc* d) {              // (the instantiation that is launched)
-  const Module m = module_of(d);
-  const bool concat = m.mix == LISA_MIX_CONCAT;
-  FfnOperands w{};
-  w.Din = m.Din;
-  w.F = m.F;
-  w.HO = d->H;
-  w.HBO = concat ? (d->H <= 16 ? 1 : d->H <= 32 ? 2 : 3) : (d->H + 15) / 16;
-  w.KS = concat ? w.HBO : (w.HBO + 1) / 2;
-  w.FS = !concat ? (m.F + 31) / 32 : m.F <= 64 ? 2 : m.F <= 128 ? 4 : 8;
-  return w;
-}
-__global__ __launch_bounds__(256) void k_cache8_operands(FfnOperands w) { ffn_operand_piece<false>(w, blockIdx.x * 256 + threadIdx.x); }
-
 // Softmax and P V: eight waves per workgroup where two pages each makes all pages of a sequence one workgroup's work, or four with as many
 // pages each as make some 4096 waves of the call (16 per compute unit).
 struct PvGeom {
@@ -141,8 +128,14 @@ PvGeom pv_geom(const lisa_desc* d) {
   return g;
 }
 
+// Pages per workgroup of the scores kernel: as many as leave some 1024 workgroups (four per compute unit).
+int scores_pages(const lisa_desc* d) {
+  const long long pages = (long long)d->B * ((d->Lk + PG_TOK - 1) / PG_TOK);
+  return (int)std::min<long long>(64, std::max<long long>(1, pages / 1024));
+}
+
 struct Ws {
-  size_t s, part_o, part_ml, img, w1, w2, total;
+  size_t s, part_o, part_ml, total;
   int Lp;
 };
 Ws ws_of(const lisa_desc* d, bool lisa_layer) {
@@ -158,16 +151,7 @@ Ws ws_of(const lisa_desc* d, bool lisa_layer) {
   const size_t parts = g.n_span > 1 ? (size_t)d->B * g.n_span * d->H : 0;
   w.part_o = take(parts * d->d_k * sizeof(float));
   w.part_ml = take(parts * 2 * sizeof(float));
-  if (lisa_layer && d->mix != LISA_MIX_SHARE) {
-    w.s = take((size_t)d->B * d->H * w.Lp * sizeof(float));
-    if (d->mix != LISA_MIX_PLUS) {
-      w.img = take((size_t)operand_shape(d).pieces() * 16);
-      if (d->act == LISA_ACT_SINGLE) {
-        w.w1 = take((size_t)module_of(d).Din * 2 * d->H * 2);
-        w.w2 = take((size_t)2 * d->H * d->H * 2);
-      }
-    }
-  }
+  if (lisa_layer && d->mix != LISA_MIX_SHARE) w.s = take((size_t)d->B * d->H * w.Lp * sizeof(float));
   w.total = std::max<size_t>(at, 256);
   return w;
 }
@@ -178,7 +162,7 @@ bool cache8_fast_ok(const lisa_desc* d, bool lisa_layer) {
   if (d->dtype != LISA_BF16 || (d->d_k != 64 && d->d_k != 128)) return false;
   if ((long long)(d->H / d->Hkv + 7) / 8 * d->Hkv > 65535) return false;
   if (!lisa_layer || d->mix == LISA_MIX_SHARE) return true;
-  if (d->r > 64 || d->H > 64) return false;
+  if (d->r > 64 || d->H > 64 || (long long)d->H * d->Lk >= 1LL << 30) return false;   // (32-bit offsets in a sequence's score rows)
   if (d->mix == LISA_MIX_PLUS) return true;
   const Module m = module_of(d);
   return d->mix == LISA_MIX_CONCAT ? d->H <= 48 && m.F <= 256 : m.F <= 128;
@@ -203,30 +187,15 @@ int run_cache8_fast(const lisa_desc* d, bool lisa_layer, int fmt, const Cache8Vi
     a.Lk = d->Lk;
     a.Lp = w.Lp;
     a.fmt = fmt;
+    a.n_pages = scores_pages(d);
     a.scale = scale;
     int rc;
     if (d->mix == LISA_MIX_PLUS) {
       rc = launch_scores_ks<1, 1, 1, 0, 0>(d, a, st);
     } else {
       const Module m = module_of(d);
-      if (d->act == LISA_ACT_SINGLE) {
-        StageScope prof("k_synth_relu_ffn", st);
-        k_synth_relu_ffn<bf16_t><<<(2 * m.Din * d->H + 2 * d->H * d->H + 255) / 256, 256, 0, st>>>(
-            (const bf16_t*)w1, (bf16_t*)(ws + w.w1), (bf16_t*)(ws + w.w2), m.Din, d->H);
-        w1 = ws + w.w1;
-        w2 = ws + w.w2;
-      }
-      FfnOperands o = operand_shape(d);
-      o.w1 = (const bf16_t*)w1;
-      o.w2 = (const bf16_t*)w2;
-      o.out = (unsigned short*)(ws + w.img);
-      {
-        StageScope prof("k_cache8_operands", st);
-        k_cache8_operands<<<(o.pieces() + 255) / 256, 256, 0, st>>>(o);
-        rc = check_launch();
-        if (rc) return rc;
-      }
-      a.img = o.out;
+      a.w1 = (const bf16_t*)w1;
+      a.w2 = d->act == LISA_ACT_SINGLE ? nullptr : (const bf16_t*)w2;
       a.F = m.F;
       rc = d->mix == LISA_MIX_CONCAT ? (m.act ? launch_cache8_concat<1>(d, a, st) : launch_cache8_concat<0>(d, a, st))
                                      : (m.act ? launch_cache8_add<1>(d, a, st) : launch_cache8_add<0>(d, a, st));
