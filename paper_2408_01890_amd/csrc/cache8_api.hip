@@ -110,6 +110,11 @@ int run_decode8(const lisa_desc* d, const lisa_cache8* cache, const void* q, con
 
 template <typename T>
 void launch_append(const Cache8View& c, bool e4m3, dim3 grid, const void* k_new, const void* v_new, const int32_t* counts, int L, hipStream_t st) {
+  if (L == 1) {
+    auto kern = e4m3 ? k_cache8_append_token<T, 1> : k_cache8_append_token<T, 0>;
+    kern<<<dim3((c.Hkv + 3) / 4, grid.z), 256, 0, st>>>(c, (const T*)k_new, (const T*)v_new, counts);
+    return;
+  }
   const bool wide = c.w > 128 || c.dk > 128;
   auto kern = e4m3 ? (wide ? k_cache8_append<T, 1, true> : k_cache8_append<T, 1, false>)
                    : (wide ? k_cache8_append<T, 0, true> : k_cache8_append<T, 0, false>);

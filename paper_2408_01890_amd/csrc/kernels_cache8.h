@@ -29,6 +29,13 @@ template <> struct code8<0> {                                // whole numbers
     const float y = rintf(__builtin_amdgcn_fmed3f(x, -127.f, 127.f));
     return (unsigned char)(x == x ? (int)y : 0);
   }
+  // four numbers within the top
+  static __device__ __forceinline__ unsigned store4(float a, float b, float c, float d, float inv) {
+    const float M = 12582912.f;                              // 1.5 * 2^23: the sum's low byte is the number rounded
+    const unsigned x = __float_as_uint(__builtin_fmaf(a, inv, M)), y = __float_as_uint(__builtin_fmaf(b, inv, M));
+    const unsigned z = __float_as_uint(__builtin_fmaf(c, inv, M)), w = __float_as_uint(__builtin_fmaf(d, inv, M));
+    return __builtin_amdgcn_perm(y, x, 0x0c0c0400u) | __builtin_amdgcn_perm(w, z, 0x04000c0cu);
+  }
 };
 template <> struct code8<1> {                                // e4m3
   static constexpr unsigned TOP_MANTISSA = 0x600000u;        // 448 = 1.75 * 2^8
@@ -37,6 +44,10 @@ template <> struct code8<1> {                                // e4m3
   static __device__ __forceinline__ unsigned char store(float x) {
     const float y = __builtin_amdgcn_fmed3f(x, -448.f, 448.f);
     return x == x ? (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 0xff) : (unsigned char)0x7f;
+  }
+  static __device__ __forceinline__ unsigned store4(float a, float b, float c, float d, float inv) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, lo, true);
   }
 };
 
@@ -63,56 +74,77 @@ struct Cache8View {
   int n_pages, max_pages, Hkv, w, w8, dk;   // w8: w rounded up to 8
   __device__ __forceinline__ unsigned char* k_block(int page, int kv) const { return k + ((size_t)page * Hkv + kv) * (w8 * PG_TOK); }
   __device__ __forceinline__ unsigned char* v_block(int page, int kv) const { return v + ((size_t)page * Hkv + kv) * (dk * PG_TOK); }
-  // The page of column `col` of sequence b; negative where there is none.
-  __device__ __forceinline__ int page_of(int b, int col) const {
-    if ((unsigned)col >= (unsigned)max_pages) return -1;
-    const int p = table[(size_t)b * max_pages + col];
-    return (unsigned)p < (unsigned)n_pages ? p : -1;
+  // The page of column `col` of sequence b; negative where there is none.  (The load does not wait for anything.)
+  __device__ __forceinline__ int entry(int b, int col) const {
+    const int p = table[(size_t)b * max_pages + min(col, max_pages - 1)];
+    return col < max_pages && (unsigned)p < (unsigned)n_pages ? p : -1;
   }
 };
 
 // ---- append -----------------------------------------------------------------------------------
-// Eight features f0 .. f0 + 7 of a row of `width` elements (zeros past the width).  Rows of whole octets are 16-byte aligned.
+// Eight features f0 .. f0 + 7 of a row of `width` elements as they lie in memory.  Rows of whole octets are 16-byte aligned.  The loads are apart
+// from what is made of them, and clamped to the row, not branched around: all of a thread's are in flight together (with
+// each octet turned into numbers where it was loaded, 6 prompts of 1500 tokens took 51 us).
 template <typename T>
-__device__ __forceinline__ void load_octet(const T* row, int f0, int width, float (&x)[8]) {
-  typedef unsigned int u32x4_ __attribute__((ext_vector_type(4)));
-  if constexpr (sizeof(T) == 4) {
+struct Octet {
+  unsigned r[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* row, int f0, int width) {
+    typedef unsigned int u32x4_ __attribute__((ext_vector_type(4)));
     if (width % 8 == 0) {
-      const float4 a = *(const float4*)(row + f0), b = *(const float4*)(row + f0 + 4);
-      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-      return;
-    }
-  } else {
-    if (width % 8 == 0) {
-      const u32x4_ a = *(const u32x4_*)(row + f0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[2 * i] = bf16_bits_to_f32(a[i] & 0xffffu), x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-      return;
-    }
-    if (width % 2 == 0) {                                    // (rows are 4-byte aligned)
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        const u32x4_ v = *(const u32x4_*)(row + f0 + 4 * h);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned a = f0 + 2 * i < width ? *(const unsigned*)(row + f0 + 2 * i) : 0u;
-        x[2 * i] = bf16_bits_to_f32(a & 0xffffu), x[2 * i + 1] = __uint_as_float(a & 0xffff0000u);
+        for (int i = 0; i < 4; ++i) r[4 * h + i] = v[i];
       }
-      return;
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = *(const unsigned*)(row + min(f0 + i, width - 1));
+    } else if (width % 2 == 0) {                             // (rows are 4-byte aligned)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = *(const unsigned*)(row + min(f0 + 2 * i, width - 2));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        r[i] = row[min(f0 + 2 * i, width - 1)].bits | (unsigned)row[min(f0 + 2 * i + 1, width - 1)].bits << 16;
     }
   }
+  // zeros past the width, and everywhere where the row is not one of the call's
+  __device__ __forceinline__ void get(int f0, int width, bool live, float (&x)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = f0 + i < width ? elem<T>::load(row + f0 + i) : 0.f;
+    for (int i = 0; i < 8; ++i) {
+      unsigned u;
+      if constexpr (sizeof(T) == 4) u = r[i];
+      else u = i & 1 ? r[i >> 1] & 0xffff0000u : r[i >> 1] << 16;
+      x[i] = live && f0 + i < width ? __uint_as_float(u) : 0.f;
+    }
+  }
+};
+// The largest magnitude as bits (infinities and NaN are the largest ones).
+__device__ __forceinline__ unsigned octet_max(const float (&x)[8], unsigned m) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+  return m;
 }
-__device__ __forceinline__ float octet_max(const float (&x)[8]) {
-  float m = 0.f;
+__device__ __forceinline__ float octet_finite_max(const float (&x)[8], float m) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(x[i]));
   return m;
 }
+// `whole`: no infinity or NaN is among the numbers (and the scale takes them all).
 template <int FMT>
-__device__ __forceinline__ unsigned long long octet_codes(const float (&x)[8], float inv) {
-  unsigned long long y = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y |= (unsigned long long)code8<FMT>::store(x[i] * inv) << (8 * i);
-  return y;
+__device__ __forceinline__ unsigned quad_codes(float a, float b, float c, float d, float inv, bool whole) {
+  typedef code8<FMT> C;
+  if (whole) return C::store4(a, b, c, d, inv);
+  return C::store(a * inv) | (unsigned)C::store(b * inv) << 8 | (unsigned)C::store(c * inv) << 16 | (unsigned)C::store(d * inv) << 24;
+}
+template <int FMT>
+__device__ __forceinline__ unsigned long long octet_codes(const float (&x)[8], float inv, bool whole) {
+  return quad_codes<FMT>(x[0], x[1], x[2], x[3], inv, whole) |
+         (unsigned long long)quad_codes<FMT>(x[4], x[5], x[6], x[7], inv, whole) << 32;
+}
+__device__ __forceinline__ unsigned wave_max_bits(unsigned v) {
+  return __float_as_uint(wave_reduce(__uint_as_float(v), [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
 }
 
 // The last counts[b] tokens of sequence b (all L rows where counts is null) go into its pages.
@@ -120,67 +152,112 @@ __device__ __forceinline__ unsigned long long octet_codes(const float (&x)[8], f
 // registers (a thread: eight features of four tokens), for the largest magnitudes and then the codes; values are turned
 // through the LDS into rows of tokens.  WIDE: rows of more than 128 features.
 constexpr int C8_VROW = PG_TOK + 4;      // bytes of a feature's row of codes in the LDS
+constexpr int C8_KROW = PG_TOK * 8 + 16;  // of an octet's
 template <typename T, int FMT, bool WIDE>
 __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __restrict__ k_new, const T* __restrict__ v_new,
                                                        const int* __restrict__ counts, int L) {
   constexpr int N = WIDE ? 2 : 1, FEATURES = N * 128;        // (16 token quads x width / 8 tasks for N * 256 threads)
   __shared__ __align__(16) unsigned char v_s[FEATURES * C8_VROW];
-  __shared__ float m_s[2][4];
+  __shared__ __align__(16) unsigned char k_s[(FEATURES / 8) * C8_KROW];
+  __shared__ unsigned m_s[2][4];
+  __shared__ float f_s[2][4];
   const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int len = c.lens[b], n_new = min(max(counts ? counts[b] : L, 0), min(L, len));
   if (n_new <= 0) return;
   const int col = (len - n_new) / PG_TOK + (int)blockIdx.x;
   if ((long long)col * PG_TOK >= len) return;
-  const int page = c.page_of(b, col);
-  if (page < 0) return;
   const int lo = max(len - n_new - col * PG_TOK, 0), hi = min(len - col * PG_TOK, PG_TOK);   // tokens of the page
-  const size_t at = (size_t)page * c.Hkv + kv;
-  const float k_old = c.w ? c.k_scale[at] : 0.f, v_old = c.v_scale[at];
   // row of token t of the page: base + t (t >= lo)
   const long long base = ((long long)b * c.Hkv + kv) * L + (col * PG_TOK - (len - n_new));
   const int nv = (c.dk + 7) / 8, nk = c.w8 / 8;
   const bool k_quads = c.w % 8 == 0;                         // else a thread has a token, three octets at most of a K_LR row keep all busy
-  float xv[N][4][8], xk[N][4][8], mk = 0.f, mv = 0.f;
+  // The rows (they are on their way while the table is asked for the page).
+  auto row_of = [&](int t) { return base + min(max(t, lo), hi - 1); };
+  auto live = [&](int t) { return t >= lo && t < hi; };
+  const int t_k = tid & 63;
+  Octet<T> rv[N][4], rk[N][4];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int e = tid + 256 * i, q = e / nv, o = e % nv;     // token quad, octet (octets fastest: rows are read on end)
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int t = 4 * q + u;
-#pragma unroll
-      for (int f = 0; f < 8; ++f) xv[i][u][f] = 0.f;
-      if (t >= lo && t < hi) load_octet(v_new + (base + t) * c.dk, 8 * o, c.dk, xv[i][u]);
-      mv = fmaxf(mv, octet_max(xv[i][u]));
-    }
+    for (int u = 0; u < 4; ++u) rv[i][u].load(v_new + row_of(4 * q + u) * c.dk, 8 * o, c.dk);
   }
-  if (k_quads) {
+  if (k_quads && nk) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = tid + 256 * i, q = nk ? e / nk : 16, o = nk ? e % nk : 0;
+      const int e = tid + 256 * i, q = e / nk, o = e % nk;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int t = 4 * q + u;
-#pragma unroll
-        for (int f = 0; f < 8; ++f) xk[i][u][f] = 0.f;
-        if (t >= lo && t < hi) load_octet(k_new + (base + t) * c.w, 8 * o, c.w, xk[i][u]);
-        mk = fmaxf(mk, octet_max(xk[i][u]));
-      }
+      for (int u = 0; u < 4; ++u) rk[i][u].load(k_new + row_of(4 * q + u) * c.w, 8 * o, c.w);
     }
-  } else {
-    for (int e = tid; e < 64 * nk; e += 256) {
-      const int t = e & 63;
-      if (t < lo || t >= hi) continue;
-      float x[8];
-      load_octet(k_new + (base + t) * c.w, 8 * (e >> 6), c.w, x);
-      mk = fmaxf(mk, octet_max(x));
+  } else if (nk) {                                           // octets tid / 64 (+ 4, ..: four of them in registers)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (4 * u < nk) rk[0][u].load(k_new + row_of(t_k) * c.w, 8 * min((tid >> 6) + 4 * u, nk - 1), c.w);
+  }
+  const int page = c.entry(b, col);
+  if (page < 0) return;
+  const size_t at = (size_t)page * c.Hkv + kv;
+  const float k_old = c.w ? c.k_scale[at] : 0.f, v_old = c.v_scale[at];
+  float xv[N][4][8], xk[N][4][8];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = tid + 256 * i;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      rv[i][u].get(8 * (e % nv), c.dk, live(4 * (e / nv) + u), xv[i][u]);
+      if (k_quads) rk[i][u].get(nk ? 8 * (e % nk) : 0, c.w, nk && live(4 * (e / nk) + u), xk[i][u]);
+      else rk[0][u].get(8 * ((tid >> 6) + 4 * u), c.w, 4 * u < nk && live(t_k), xk[0][u]);
     }
   }
-  mk = wave_max(mk), mv = wave_max(mv);
+  unsigned mk = 0, mv = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      mv = octet_max(xv[i][u], mv);
+      if (i == 0 || k_quads) mk = octet_max(xk[i][u], mk);
+    }
+  if (!k_quads)                                              // (rows of more than 128 features)
+    for (int o = (tid >> 6) + 16; o < nk; o += 4)
+      if (live(t_k)) {
+        float x[8];
+        Octet<T> r;
+        r.load(k_new + row_of(t_k) * c.w, 8 * o, c.w);
+        r.get(8 * o, c.w, true, x);
+        mk = octet_max(x, mk);
+      }
+  mk = wave_max_bits(mk), mv = wave_max_bits(mv);
   if ((tid & 63) == 0) m_s[0][tid >> 6] = mk, m_s[1][tid >> 6] = mv;
   __syncthreads();
-  mk = fmaxf(fmaxf(m_s[0][0], m_s[0][1]), fmaxf(m_s[0][2], m_s[0][3]));
-  mv = fmaxf(fmaxf(m_s[1][0], m_s[1][1]), fmaxf(m_s[1][2], m_s[1][3]));
-  float k_now = block_scale<FMT>(mk), v_now = block_scale<FMT>(mv);
+  mk = max(max(m_s[0][0], m_s[0][1]), max(m_s[0][2], m_s[0][3]));
+  mv = max(max(m_s[1][0], m_s[1][1]), max(m_s[1][2], m_s[1][3]));
+  const bool k_whole = mk < 0x7f800000u, v_whole = mv < 0x7f800000u;
+  float fk = __uint_as_float(mk), fv = __uint_as_float(mv);
+  if (!(k_whole && v_whole)) {                               // the largest finite magnitudes
+    fk = 0.f, fv = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        fv = octet_finite_max(xv[i][u], fv);
+        if (i == 0 || k_quads) fk = octet_finite_max(xk[i][u], fk);
+      }
+    if (!k_quads)
+      for (int o = (tid >> 6) + 16; o < nk; o += 4)
+        if (live(t_k)) {
+          float x[8];
+          Octet<T> r;
+          r.load(k_new + row_of(t_k) * c.w, 8 * o, c.w);
+          r.get(8 * o, c.w, true, x);
+          fk = octet_finite_max(x, fk);
+        }
+    fk = wave_max(fk), fv = wave_max(fv);
+    if ((tid & 63) == 0) f_s[0][tid >> 6] = fk, f_s[1][tid >> 6] = fv;
+    __syncthreads();
+    fk = fmaxf(fmaxf(f_s[0][0], f_s[0][1]), fmaxf(f_s[0][2], f_s[0][3]));
+    fv = fmaxf(fmaxf(f_s[1][0], f_s[1][1]), fmaxf(f_s[1][2], f_s[1][3]));
+  }
+  float k_now = block_scale<FMT>(fk), v_now = block_scale<FMT>(fv);
   if (lo) k_now = fmaxf(k_now, k_old), v_now = fmaxf(v_now, v_old);   // (tokens that are there already count too)
   if (tid == 0) {
     if (c.w) c.k_scale[at] = k_now;
@@ -194,12 +271,9 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __
     const int e = tid + 256 * i, q = e / nv, o = e % nv;
     if (q >= 16 || 4 * q >= hi || 4 * q + 4 <= lo) continue;
 #pragma unroll
-    for (int f = 0; f < 8; ++f) {
-      unsigned y = 0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) y |= (unsigned)Code::store(xv[i][u][f] * v_inv) << (8 * u);
-      if (8 * o + f < c.dk) *(unsigned*)(v_s + (8 * o + f) * C8_VROW + 4 * q) = y;
-    }
+    for (int f = 0; f < 8; ++f)
+      if (8 * o + f < c.dk)
+        *(unsigned*)(v_s + (8 * o + f) * C8_VROW + 4 * q) = quad_codes<FMT>(xv[i][0][f], xv[i][1][f], xv[i][2][f], xv[i][3][f], v_inv, v_whole);
   }
   // keys: 8 features of a token at a time
   unsigned char* kb = c.k_block(page, kv);
@@ -211,16 +285,21 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int t = 4 * q + u;
-        if (t >= lo && t < hi) *(unsigned long long*)(kb + (o * PG_TOK + t) * 8) = octet_codes<FMT>(xk[i][u], k_inv);
+        if (t >= lo && t < hi) *(unsigned long long*)(k_s + o * C8_KROW + t * 8) = octet_codes<FMT>(xk[i][u], k_inv, k_whole);
       }
     }
-  } else {
-    for (int e = tid; e < 64 * nk; e += 256) {
-      const int t = e & 63;
-      if (t < lo || t >= hi) continue;
+  } else if (live(t_k)) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int o = (tid >> 6) + 4 * u;
+      if (o < nk) *(unsigned long long*)(kb + (o * PG_TOK + t_k) * 8) = octet_codes<FMT>(xk[0][u], k_inv, k_whole);
+    }
+    for (int o = (tid >> 6) + 16; o < nk; o += 4) {
       float x[8];
-      load_octet(k_new + (base + t) * c.w, 8 * (e >> 6), c.w, x);
-      *(unsigned long long*)(kb + ((e >> 6) * PG_TOK + t) * 8) = octet_codes<FMT>(x, k_inv);
+      Octet<T> r;
+      r.load(k_new + row_of(t_k) * c.w, 8 * o, c.w);
+      r.get(8 * o, c.w, true, x);
+      *(unsigned long long*)(kb + (o * PG_TOK + t_k) * 8) = octet_codes<FMT>(x, k_inv, k_whole);
     }
   }
   if (lo && k_now > k_old)
@@ -233,6 +312,18 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __
       *at8 = y;
     }
   __syncthreads();
+  if (k_quads)                                               // out as rows of tokens, two at a time
+    for (int e = tid; e < nk * 32; e += 256) {
+      const int o = e >> 5, t = 2 * (e & 31);
+      const unsigned long long* src = (const unsigned long long*)(k_s + o * C8_KROW + t * 8);
+      unsigned long long* dst = (unsigned long long*)(kb + (o * PG_TOK + t) * 8);
+      if (t >= lo && t + 2 <= hi) {
+        *(uint4*)dst = *(const uint4*)src;
+      } else {
+        if (t >= lo && t < hi) dst[0] = src[0];
+        if (t + 1 >= lo && t + 1 < hi) dst[1] = src[1];
+      }
+    }
   unsigned char* vb = c.v_block(page, kv);
   const int from = lo && v_now > v_old ? 0 : lo;              // tokens to write
   if (from < lo) {
@@ -254,6 +345,58 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8View c, const T* __
   }
 }
 
+// One new token per sequence (L = 1): a wave has a head of a sequence, so nothing waits for other waves: what it takes is the chain lens ->
+// table -> scales -> codes.  grid (ceil(Hkv / 4), B), block 256.  (64 sequences, 32 heads: 17.8 us with k_cache8_append, whose threads all load.)
+template <typename T, int FMT>
+__global__ __launch_bounds__(256) void k_cache8_append_token(Cache8View c, const T* __restrict__ k_new, const T* __restrict__ v_new,
+                                                             const int* __restrict__ counts) {
+  typedef code8<FMT> Code;
+  constexpr int E = 4;                                       // elements of a row per lane (256 features at most)
+  const int lane = threadIdx.x & 63, kv = blockIdx.x * 4 + (threadIdx.x >> 6), b = blockIdx.y;
+  if (kv >= c.Hkv) return;
+  const size_t row = (size_t)b * c.Hkv + kv;
+  float xk[E], xv[E], mk = 0.f, mv = 0.f;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int f = lane + 64 * i;
+    xk[i] = f < c.w ? elem<T>::load(k_new + row * c.w + f) : 0.f;
+    xv[i] = f < c.dk ? elem<T>::load(v_new + row * c.dk + f) : 0.f;
+  }
+  const int len = c.lens[b], col = (len - 1) / PG_TOK, t = (len - 1) % PG_TOK;
+  if (len <= 0 || (counts && counts[b] <= 0)) return;
+  const int page = c.entry(b, col);
+  if (page < 0) return;
+  const size_t at = (size_t)page * c.Hkv + kv;
+  const float k_old = c.w ? c.k_scale[at] : 0.f, v_old = c.v_scale[at];
+#pragma unroll
+  for (int i = 0; i < E; ++i) mk = fmaxf(mk, finite_abs(xk[i])), mv = fmaxf(mv, finite_abs(xv[i]));
+  float k_now = block_scale<FMT>(wave_max(mk)), v_now = block_scale<FMT>(wave_max(mv));
+  if (t) k_now = fmaxf(k_now, k_old), v_now = fmaxf(v_now, v_old);
+  if (lane == 0) {
+    if (c.w) c.k_scale[at] = k_now;
+    c.v_scale[at] = v_now;
+  }
+  const float k_inv = 1.f / k_now, v_inv = 1.f / v_now;
+  unsigned char* kb = c.k_block(page, kv);
+  unsigned char* vb = c.v_block(page, kv);
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int f = lane + 64 * i;
+    if (f < c.w8) kb[((f >> 3) * PG_TOK + t) * 8 + (f & 7)] = Code::store(xk[i] * k_inv);   // (past the width: zeros)
+    if (f < c.dk) vb[f * PG_TOK + t] = Code::store(xv[i] * v_inv);
+  }
+  if (t && k_now > k_old)                                    // the tokens in front, rounded again
+    for (int e = lane; e < c.w8 * t; e += 64) {
+      unsigned char* p = kb + ((e / (8 * t)) * PG_TOK + e / 8 % t) * 8 + (e & 7);
+      *p = Code::store(Code::load(*p) * k_old * k_inv);
+    }
+  if (t && v_now > v_old)
+    for (int e = lane; e < c.dk * t; e += 64) {
+      unsigned char* p = vb + (e / t) * PG_TOK + e % t;
+      *p = Code::store(Code::load(*p) * v_old * v_inv);
+    }
+}
+
 // ---- decode step, any shape ---------------------------------------------------------------------
 // Scores of one page (64 keys) of one sequence, all heads; float32 arithmetic.  The stages of k_lisa_scores; `mix` 4: the
 // standard layer's q K^T.  exact [B][H][Lk] float32, -inf at keys that have no page; `scores` may be null.
@@ -273,7 +416,7 @@ __global__ __launch_bounds__(256) void k_cache8_scores(Cache8View c, const T* __
   const int pj = threadIdx.x & 63, sl = threadIdx.x >> 6;
   const int j = col * PG_TOK + pj;
   if (col * PG_TOK >= len) return;
-  const int page = c.page_of(b, col);
+  const int page = c.entry(b, col);
   const bool live = j < len && page >= 0;
   const int group = H / c.Hkv;
   const size_t row = (size_t)b * H * Lk + j;                 // + h * Lk
@@ -328,7 +471,7 @@ __global__ __launch_bounds__(256) void k_cache8_softmax_v(Cache8View c, const fl
   const float* a = exact + ((size_t)b * H + h) * Lk;
   float m_run = -INFINITY, l_run = 0.f, acc = 0.f;           // (m_run, l_run: the first wave)
   for (int col = 0; col * PG_TOK < len; ++col) {
-    const int page = c.page_of(b, col);
+    const int page = c.entry(b, col);
     if (page < 0) continue;                                  // (uniform)
     if (tid < 64) {
       const int j = col * PG_TOK + tid;

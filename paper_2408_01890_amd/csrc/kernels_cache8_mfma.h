@@ -335,9 +335,9 @@ __global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col0 = blockIdx.x * a.n_pages, b = blockIdx.y;
-  const int len = min(c.lens[b], a.Lk);
   const int my_col = col0 + lane;                            // lane i: the workgroup's page i
-  const int id = lane < a.n_pages && (long long)my_col * PG_TOK < len ? c.page_of(b, my_col) : -1;
+  const int entry = c.entry(b, my_col), len = min(c.lens[b], a.Lk);
+  const int id = lane < a.n_pages && (long long)my_col * PG_TOK < len ? entry : -1;
   unsigned long long todo = __ballot(id >= 0);
   if (!todo) return;
   const int n = lane & 15, g = lane >> 4;
@@ -557,12 +557,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && GT == 1 && GH == 1 && MODE < 2 
   const int b = blockIdx.z, span = blockIdx.y, kv = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
   const int group = a.H / c.Hkv, h0 = chunk * 4 * GT, heads = min(4 * GT, group - h0);   // heads of this workgroup
   const int head0 = kv * group + h0;
-  const int len = max(min(c.lens[b], a.Lk), 0), n_pages = (len + PG_TOK - 1) / PG_TOK;
-  const int p_begin = span * a.span_pages, p_end = min(n_pages, p_begin + a.span_pages);
-  if (p_begin >= n_pages && a.n_span > 1) return;            // (k_cache8_combine knows)
   // lane i: page p_begin + wv + NW i (span_pages <= 64 NW)
-  const int my_col = p_begin + wv + NW * lane;
-  const int id = my_col < p_end ? c.page_of(b, my_col) : -1;
+  const int p_begin = span * a.span_pages, my_col = p_begin + wv + NW * lane;
+  const int entry = c.entry(b, my_col), len = max(min(c.lens[b], a.Lk), 0);
+  const int n_pages = (len + PG_TOK - 1) / PG_TOK, p_end = min(n_pages, p_begin + a.span_pages);
+  if (p_begin >= n_pages && a.n_span > 1) return;            // (k_cache8_combine knows)
+  const int id = my_col < p_end ? entry : -1;
   const size_t id_at = (size_t)max(id, 0) * c.Hkv + kv;
   const float ksc = MODE == 0 ? c.k_scale[id_at] : 0.f, vsc = c.v_scale[id_at];
   unsigned long long todo = __ballot(id >= 0);
