@@ -542,7 +542,7 @@ struct Cache8PvArgs {
 // 8 or 16 KB of a step.
 // GT: tiles of four query heads, GH: heads of a tile that are there (1: one query head per key/value head).
 template <int FMT, int DK, int MODE, int GT, int GH, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 4 && GT == 1 && GH == 1 && MODE < 2 ? (MODE == 1 ? 4 : 3) : 1) void k_cache8_pv(Cache8PvArgs a) {
+__global__ __launch_bounds__(64 * NW, MODE == 0 && NW == 4 && GT == 1 && GH == 1 ? 3 : 1) void k_cache8_pv(Cache8PvArgs a) {
   typedef mfma8<FMT> M;
   constexpr int KS = DK / 32, NT = DK / 16;
   constexpr float LOG2E = 1.4426950408889634f;

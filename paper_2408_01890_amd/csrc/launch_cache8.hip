@@ -71,7 +71,8 @@ template <int FMT, int DK, int MODE, int GT, int GH>
 int launch_pv_nw(const lisa_desc* d, int wide, const Cache8PvArgs& a, hipStream_t st) {
   const dim3 grid(d->Hkv * a.chunks, a.n_span, d->B);
   StageScope prof("k_cache8_pv", st);
-  if (wide) k_cache8_pv<FMT, DK, MODE, GT, GH, 8><<<grid, 512, 0, st>>>(a);
+  constexpr bool EIGHT = MODE > 0 && GT == 1;                // (pv_geom)
+  if (EIGHT && wide) k_cache8_pv<FMT, DK, MODE, GT, GH, EIGHT ? 8 : 4><<<grid, 512, 0, st>>>(a);
   else k_cache8_pv<FMT, DK, MODE, GT, GH, 4><<<grid, 256, 0, st>>>(a);
   return check_launch();
 }
@@ -110,20 +111,25 @@ Module module_of(const lisa_desc* d) {
   m.act = d->act == LISA_ACT_SILU ? 1 : 0;
   return m;
 }
-// Softmax and P V: eight waves per workgroup where two pages each makes all pages of a sequence one workgroup's work, or four with as many
-// pages each as make some 4096 waves of the call (16 per compute unit).
+// Softmax and P V: what a workgroup spends before its first page and after its last (page numbers, scales and queries; merging its waves) is
+// some five pages' time, so a (sequence, kv head) is one workgroup's work where that makes 256 of them, one per compute unit; else it
+// is split until there are, down to 16 pages.  Eight waves for LiSA layers: a stream of V runs best with few of them per compute unit
+// (64 sequences of up to 4097 tokens, 32 heads: 192 us for the layer, 223 with four such workgroups of four waves per compute unit).
+// Four for standard layers (fewer leave their registers room; 32 sequences of up to 8192, 8 kv heads: 76 us, 85 at eight spans instead of one),
+// where a wave has more than four heads (256 registers do not hold them with eight) and where several workgroups per compute unit with 32
+// pages at most follow one another (64 sequences of up to 500 tokens, 32 heads: 35 us, with eight 43; at 2500 129 and 126).
 struct PvGeom {
   int wide, span_pages, n_span, chunks;
 };
-PvGeom pv_geom(const lisa_desc* d) {
-  const int group = d->H / d->Hkv, n_pages = (d->Lk + PG_TOK - 1) / PG_TOK;
+PvGeom pv_geom(const lisa_desc* d, bool lisa_layer) {
+  const int group = d->H / d->Hkv, n_pages = std::max((d->Lk + PG_TOK - 1) / PG_TOK, 1);
   PvGeom g;
   g.chunks = group <= 4 ? 1 : (group + 7) / 8;
   const long long base = (long long)d->B * d->Hkv * g.chunks;
-  const int per_wave = (int)std::min<long long>(64, std::max<long long>(1, base * n_pages / 4096));
-  g.wide = base * ((n_pages + 15) / 16) <= 512 || n_pages <= 16;
-  if (base >= 1024) g.wide = 0;
-  g.span_pages = std::min(g.wide ? std::max(16, 8 * per_wave) : 4 * per_wave, (n_pages + 3) / 4 * 4);
+  g.wide = lisa_layer && group <= 4 && (base < 512 || n_pages > 32);
+  const int waves = g.wide ? 8 : 4;
+  const int spans = (int)std::max<long long>(1, std::min<long long>((256 + base - 1) / base, (n_pages + 15) / 16));
+  g.span_pages = std::min((int)round_up((n_pages + spans - 1) / spans, waves), 64 * waves);
   g.n_span = (n_pages + g.span_pages - 1) / g.span_pages;
   return g;
 }
@@ -139,7 +145,7 @@ struct Ws {
   int Lp;
 };
 Ws ws_of(const lisa_desc* d, bool lisa_layer) {
-  const PvGeom g = pv_geom(d);
+  const PvGeom g = pv_geom(d, lisa_layer);
   Ws w{};
   w.Lp = (d->Lk + PG_TOK - 1) / PG_TOK * PG_TOK;
   size_t at = 0;
@@ -173,7 +179,7 @@ size_t cache8_fast_bytes(const lisa_desc* d, bool lisa_layer) { return ws_of(d, 
 int run_cache8_fast(const lisa_desc* d, bool lisa_layer, int fmt, const Cache8View& c, const void* q, const void* prev, const void* w1,
                     const void* w2, float scale, void* row, void* out, void* workspace, hipStream_t st) {
   const Ws w = ws_of(d, lisa_layer);
-  const PvGeom g = pv_geom(d);
+  const PvGeom g = pv_geom(d, lisa_layer);
   char* ws = (char*)workspace;
   const bool share = lisa_layer && d->mix == LISA_MIX_SHARE;
   if (lisa_layer && !share) {
