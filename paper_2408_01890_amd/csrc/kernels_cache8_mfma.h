@@ -312,9 +312,6 @@ struct FfnStage {
   }
 };
 
-#ifndef C8_SCORES_WAVES
-#define C8_SCORES_WAVES(MODE, KVT, KS) 2
-#endif
 // MODE 0: A_n = A_{n-1} + A_delta, 1: FFN(A_{n-1}) + A_delta, 2: FFN([A_{n-1}; A_delta]).  KS: pieces of 32 features of a K_LR row.
 // grid (ceil(pages / n_pages), B), block 256: n_pages pages of a sequence, all heads.  Per page the waves take tiles of four heads in turn
 // (A_delta to the LDS), then 16 tokens each through the FFN; the next page's keys and A_{n-1} are loaded where this one's have been used, and one
@@ -322,9 +319,9 @@ struct FfnStage {
 // KVT: key/value heads that the four heads of a tile can have, 1 (groups of whole tiles) or 4; their products go into one accumulator, so that what
 // follows on the vector ALU (16 sums over the pieces) is done once per tile.
 template <int HBI, int FS, int HBO, int ACT, int MODE, int KS, int KVT>
-__global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_scores_mfma(Cache8ScoresArgs a) {
+__global__ __launch_bounds__(256, 2) void k_cache8_scores_mfma(Cache8ScoresArgs a) {
   typedef MfmaFfn<HBI, FS, HBO, ACT> Ffn;
-  constexpr int KX = MODE == 0 ? 1 : Ffn::KS;
+  constexpr int KX = MODE == 0 ? 1 : Ffn::KS, KP = MODE == 2 ? (KX + 1) / 2 : KX;   // pieces of 32 channels, those with A_{n-1}
   extern __shared__ __align__(16) float c8_lds[];
   const Cache8View& c = a.c;
   const int H = a.H, Din = MODE == 2 ? 2 * H : H;
@@ -371,13 +368,13 @@ __global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_
   };
   // A_{n-1} of this lane's token: what the FFN takes (clamped; past the heads and the end it is zeroed where it is used).  One element per
   // register: to pack them is to wait for them.
-  unsigned short xin[KX][8];
+  unsigned short xin[KP][8];
   auto load_x = [&](int i) {
     const unsigned short* xp = (const unsigned short*)a.prev + (size_t)b * H * a.Lk;   // (32-bit offsets: H Lk < 2^30)
     const unsigned j = min((col0 + i) * PG_TOK + pj, len - 1);
     if (MODE != 0)
 #pragma unroll
-      for (int ks = 0; ks < KX; ++ks)
+      for (int ks = 0; ks < KP; ++ks)
 #pragma unroll
         for (int e = 0; e < 8; ++e) xin[ks][e] = xp[(unsigned)min(32 * ks + 8 * g + e, H - 1) * (unsigned)a.Lk + j];
   };
@@ -386,11 +383,6 @@ __global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_
   qst.load(0, H, c.w, tid, src);
   FfnStage<KX, FS, HBO> fst;
   if (MODE != 0) fst.load(a, Din, tid);
-  if (MODE == 2) {                                           // (a wide network: its registers first)
-    __builtin_amdgcn_sched_barrier(0);
-    fst.store(a, Din, w_s, tid);
-    __builtin_amdgcn_sched_barrier(0);
-  }
   int at = __builtin_ctzll(todo), buf = 0;
   {
     const int page = __builtin_amdgcn_readlane(id, at);
@@ -399,7 +391,7 @@ __global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_
     load_x(at);
   }
   qst.store(a.fmt, H, c.w, q_s, e_s, tid, 256, src);
-  if (MODE == 1) fst.store(a, Din, w_s, tid);
+  if (MODE != 0) fst.store(a, Din, w_s, tid);
   lds_barrier();
   auto delta = [&](auto fmt, int tile, const Tile& t, float* to) __attribute__((always_inline)) {
     constexpr int FMT = decltype(fmt)::value;
@@ -478,14 +470,17 @@ __global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_
         emit(h, y);
       }
     } else {
+      // (what follows from the lane's number is made anew: kept over the pages, it does not fit the registers)
+      int go = g, po = pj;
+      if (MODE == 2) asm volatile("" : "+v"(go), "+v"(po));
       f16x8 x[1][KX];
 #pragma unroll
       for (int ks = 0; ks < KX; ++ks)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int ch = 32 * ks + 8 * g + e;
-          x[0][ks][e] = __builtin_bit_cast(half_t, xin[ks][e]);
-          if (MODE == 2 && ch >= H) x[0][ks][e] = ch < Din ? f32_to_half_sat(to[(ch - H) * C8_SROW + pj]) : (_Float16)0.f;
+          const int ch = 32 * ks + 8 * go + e;
+          x[0][ks][e] = ks < KP ? __builtin_bit_cast(half_t, xin[ks < KP ? ks : 0][e]) : (_Float16)0.f;
+          if (MODE == 2 && ch >= H) x[0][ks][e] = ch < Din ? f32_to_half_sat(to[(ch - H) * C8_SROW + po]) : (_Float16)0.f;
           else if (ch >= Din) x[0][ks][e] = (_Float16)0.f;
         }
       if (MORE) load_x(next);
@@ -497,12 +492,12 @@ __global__ __launch_bounds__(256, C8_SCORES_WAVES(MODE, KVT, KS)) void k_cache8_
 #pragma unroll
       for (int hb = 0; hb < HBO; ++hb)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) d[hb][v] = MODE == 2 ? 0.f : to[min(16 * hb + 4 * g + v, H) * C8_SROW + pj];
+        for (int v = 0; v < 4; ++v) d[hb][v] = MODE == 2 ? 0.f : to[min(16 * hb + 4 * go + v, H) * C8_SROW + po];
 #pragma unroll
       for (int hb = 0; hb < HBO; ++hb)
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          to[min(16 * hb + 4 * g + v, H) * C8_SROW + pj] = y[0][hb][v] + d[hb][v];
+          to[min(16 * hb + 4 * go + v, H) * C8_SROW + po] = y[0][hb][v] + d[hb][v];
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int hb = 0; hb < HBO; ++hb)

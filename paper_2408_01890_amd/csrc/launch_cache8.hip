@@ -7,7 +7,7 @@ namespace lisa {
 
 namespace {
 template <int HBI, int FS, int HBO, int ACT, int MODE, int KS, int KVT>
-int launch_scores_t(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t st) {
+int launch_scores_t(const lisa_desc* d, Cache8ScoresArgs a, hipStream_t st) {
   const int lds = cache8_scores_lds(d->H, KS, MODE == 0 ? 0 : MfmaFfn<HBI, FS, HBO, ACT>::kStageBytes);
   auto kern = k_cache8_scores_mfma<HBI, FS, HBO, ACT, MODE, KS, KVT>;
   if (lds > 64 * 1024) {
@@ -15,7 +15,12 @@ int launch_scores_t(const lisa_desc* d, const Cache8ScoresArgs& a, hipStream_t s
     if (e != hipSuccess) return hip_fail(e);
   }
   StageScope prof("k_cache8_scores_mfma", st);
-  const int pages = (d->Lk + PG_TOK - 1) / PG_TOK;
+  // Pages per workgroup: as few as leave no more workgroups than the card holds at once (queries and weights are staged once per workgroup, and
+  // a second round of workgroups would be as long as the first).  64 sequences of up to 4097 tokens, 32 heads, us for the layer: ADD 192, with
+  // half as many pages 195, with twice as many 221.
+  constexpr int PER_CU = MODE < 2 && KVT == 1 && HBI <= 2 ? 3 : 2;   // by registers
+  const int pages = (d->Lk + PG_TOK - 1) / PG_TOK, room = std::max(1, kComputeUnits * std::min(PER_CU, 160 * 1024 / lds) / d->B);   // workgroups per sequence
+  a.n_pages = std::min(64, (pages + room - 1) / room);
   kern<<<dim3((pages + a.n_pages - 1) / a.n_pages, d->B), 256, lds, st>>>(a);
   return check_launch();
 }
@@ -134,12 +139,6 @@ PvGeom pv_geom(const lisa_desc* d, bool lisa_layer) {
   return g;
 }
 
-// Pages per workgroup of the scores kernel: as many as leave some 1024 workgroups (four per compute unit).
-int scores_pages(const lisa_desc* d) {
-  const long long pages = (long long)d->B * ((d->Lk + PG_TOK - 1) / PG_TOK);
-  return (int)std::min<long long>(64, std::max<long long>(1, pages / 1024));
-}
-
 struct Ws {
   size_t s, part_o, part_ml, total;
   int Lp;
@@ -193,7 +192,6 @@ int run_cache8_fast(const lisa_desc* d, bool lisa_layer, int fmt, const Cache8Vi
     a.Lk = d->Lk;
     a.Lp = w.Lp;
     a.fmt = fmt;
-    a.n_pages = scores_pages(d);
     a.scale = scale;
     int rc;
     if (d->mix == LISA_MIX_PLUS) {
