@@ -776,27 +776,43 @@ __global__ __launch_bounds__(64 * NW, MODE == 0 && NW == 4 && GT == 1 && GH == 1
   }
 }
 
-// out = the spans of a sequence merged.  grid (H, B), block DK.
+// out = the spans of a sequence merged.  grid (H, B), block DK.  A lane has a span's maximum and sum, 64 at a time; loads of eight spans in flight.
 template <int DK>
 __global__ __launch_bounds__(DK) void k_cache8_combine(const float* __restrict__ part_o, const float* __restrict__ part_ml,
                                                        const int* __restrict__ lens, void* __restrict__ out, int H, int Lk, int n_span,
                                                        int span_tokens, int out_f32) {
   constexpr float LOG2E = 1.4426950408889634f;
-  const int h = blockIdx.x, b = blockIdx.y, f = threadIdx.x;
+  const int h = blockIdx.x, b = blockIdx.y, f = threadIdx.x, lane = f & 63;
   const int len = max(min(lens[b], Lk), 0), n = (len + span_tokens - 1) / span_tokens;
   const size_t at = (size_t)b * n_span * H + h;
-  float mm = -INFINITY;
-  for (int s = 0; s < n; ++s) {
-    const float2 ml = *(const float2*)(part_ml + (at + (size_t)s * H) * 2);
-    if (ml.y != 0.f) mm = fmaxf(mm, ml.x);
-  }
-  float num = 0.f, den = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const float2 ml = *(const float2*)(part_ml + (at + (size_t)s * H) * 2);
-    const float k = ml.y != 0.f ? fast_exp2((ml.x - mm) * LOG2E) : 0.f;
-    num += k * part_o[(at + (size_t)s * H) * DK + f];
-    den += k * ml.y;
+  float mm = -INFINITY, num = 0.f, den = 0.f;
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    const int mine = min(s0 + lane, n - 1);
+    const float2 ml = *(const float2*)(part_ml + (at + (size_t)mine * H) * 2);
+    const bool in = s0 + lane < n && ml.y != 0.f;
+    float m = in ? ml.x : -INFINITY;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    m = fmaxf(m, mm);
+    if (m == -INFINITY) continue;                            // (no key yet)
+    const float alpha = fast_exp2((mm - m) * LOG2E), k = in ? fast_exp2((ml.x - m) * LOG2E) : 0.f;
+    float l = in ? k * ml.y : 0.f;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
+    mm = m;
+    den = den * alpha + l;
+    num *= alpha;
+    const int cnt = min(64, n - s0);
+    for (int s = 0; s < cnt; s += 8) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = part_o[(at + (size_t)(s0 + min(s + u, cnt - 1)) * H) * DK + f];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k), min(s + u, 63)));
+        if (s + u < cnt) num += w * x[u];
+      }
+    }
   }
   const float y = den == 0.f ? 0.f : num / den;
   if (out_f32) ((float*)out)[((size_t)b * H + h) * DK + f] = y;

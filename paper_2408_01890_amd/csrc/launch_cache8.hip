@@ -118,7 +118,8 @@ Module module_of(const lisa_desc* d) {
 }
 // Softmax and P V: what a workgroup spends before its first page and after its last (page numbers, scales and queries; merging its waves) is
 // some five pages' time, so a (sequence, kv head) is one workgroup's work where that makes 256 of them, one per compute unit; else it
-// is split until there are, down to 16 pages.  Eight waves for LiSA layers: a stream of V runs best with few of them per compute unit
+// is split until there are, more than 16 pages into eights at the smallest (a launch more, some 3 us; LiSA, one sequence of 3000 tokens, 8 kv heads:
+// 16.0 us, unsplit 21.5; of 1000: 15.9 and 14.7).  Eight waves for LiSA layers: a stream of V runs best with few of them per compute unit
 // (64 sequences of up to 4097 tokens, 32 heads: 192 us for the layer, 223 with four such workgroups of four waves per compute unit).
 // Four for standard layers (fewer leave their registers room; 32 sequences of up to 8192, 8 kv heads: 76 us, 85 at eight spans instead of one),
 // where a wave has more than four heads (256 registers do not hold them with eight) and where several workgroups per compute unit with 32
@@ -133,7 +134,7 @@ PvGeom pv_geom(const lisa_desc* d, bool lisa_layer) {
   const long long base = (long long)d->B * d->Hkv * g.chunks;
   g.wide = lisa_layer && group <= 4 && (base < 512 || n_pages > 32);
   const int waves = g.wide ? 8 : 4;
-  const int spans = (int)std::max<long long>(1, std::min<long long>((256 + base - 1) / base, (n_pages + 15) / 16));
+  const int spans = n_pages <= 16 ? 1 : (int)std::min<long long>((256 + base - 1) / base, (n_pages + 7) / 8);
   g.span_pages = std::min((int)round_up((n_pages + spans - 1) / spans, waves), 64 * waves);
   g.n_span = (n_pages + g.span_pages - 1) / g.span_pages;
   return g;
