@@ -522,16 +522,17 @@ struct Cache8PvArgs {
   const float* s;         // MODE 1: A_n [B][pages][H][64]
   const half_t* prev;     // MODE 2: A_n [B,H,Lk]
   half_t* row;            // MODE 0, 2: A_n out [B,H,Lk] or null
-  void* out;              // [B,H,DK]
-  float* part_o;          // [B][n_span][H][DK]   (n_span > 1)
+  void* out;              // [B,H,d_k]
+  float* part_o;          // [B][n_span][H][d_k]   (n_span > 1)
   float* part_ml;         // [B][n_span][H][2]
   int H, Lk, Lp, n_span, span_pages, out_f32;
   int chunks;             // workgroups that the query heads of a key/value head are dealt to, 4 GT each
+  int f_parts;            // MODE 1, 2: workgroups that its features are dealt to, DK each
   float scale;
 };
 
 // MODE 0: a standard layer (scores from K), 1: scores given in float32, 2: in half, emitted as they are.
-// grid (Hkv chunks, n_span, B), block 64 NW: the pages of a span are dealt to the waves, each with softmax state and sums of its own,
+// DK: features of a workgroup (MODE 0: d_k).  grid (Hkv chunks f_parts, n_span, B), block 64 NW: the pages of a span are dealt to the waves, each with softmax state and sums of its own,
 // merged through the LDS at the end; spans by k_cache8_combine.  Bound: the stream of K and V (a page of a head is loaded where the
 // one before it has been used, so that every wave has loads in flight); the vector ALU needs 100 - 200 instructions for the
 // 8 or 16 KB of a step.
@@ -549,7 +550,9 @@ __global__ __launch_bounds__(64 * NW, MODE == 0 && NW == 4 && GT == 1 && GH == 1
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4, hn = n & 3, pc = n >> 2;
-  const int b = blockIdx.z, span = blockIdx.y, kv = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+  const int dk = MODE == 0 ? DK : c.dk, f0 = MODE == 0 ? 0 : blockIdx.x % a.f_parts * DK;
+  const int kvc = MODE == 0 ? blockIdx.x : blockIdx.x / a.f_parts;
+  const int b = blockIdx.z, span = blockIdx.y, kv = kvc / a.chunks, chunk = kvc % a.chunks;
   const int group = a.H / c.Hkv, h0 = chunk * 4 * GT, heads = min(4 * GT, group - h0);   // heads of this workgroup
   const int head0 = kv * group + h0;
   // lane i: page p_begin + wv + NW i (span_pages <= 64 NW)
@@ -575,7 +578,7 @@ __global__ __launch_bounds__(64 * NW, MODE == 0 && NW == 4 && GT == 1 && GH == 1
     }
   };
   auto load_v = [&](int i) {
-    const unsigned char* vb = c.v_block(__builtin_amdgcn_readlane(id, i), kv) + n * PG_TOK + 16 * g;
+    const unsigned char* vb = c.v_block(__builtin_amdgcn_readlane(id, i), kv) + (f0 + n) * PG_TOK + 16 * g;
 #pragma unroll
     for (int t = 0; t < NT; ++t) vreg[t] = c8_stream(vb + t * (16 * PG_TOK));
   };
@@ -656,7 +659,7 @@ __global__ __launch_bounds__(64 * NW, MODE == 0 && NW == 4 && GT == 1 && GH == 1
     }
 #pragma unroll
     for (int t = 0; t < GT; ++t) {
-      if (MODE != 1 && a.row && 4 * t + hn < heads) {        // lane (head, quarter, g): four of its sixteen tokens
+      if (MODE != 1 && a.row && 4 * t + hn < heads && f0 == 0) {        // lane (head, quarter, g): four of its sixteen tokens
         float z[4];
         quarter(x[t], pc, z);
         half_t y[4];
@@ -765,11 +768,11 @@ __global__ __launch_bounds__(64 * NW, MODE == 0 && NW == 4 && GT == 1 && GH == 1
     const int h = head0 + hl;
     if (a.n_span > 1) {
       const size_t at = ((size_t)b * a.n_span + span) * a.H + h;
-      a.part_o[at * DK + f] = num;
-      if (f == 0) a.part_ml[at * 2] = m0, a.part_ml[at * 2 + 1] = den;
+      a.part_o[at * dk + f0 + f] = num;
+      if (f0 + f == 0) a.part_ml[at * 2] = m0, a.part_ml[at * 2 + 1] = den;
     } else {
       const float y = den == 0.f ? 0.f : num / den;
-      const size_t at = ((size_t)b * a.H + h) * DK + f;
+      const size_t at = ((size_t)b * a.H + h) * dk + f0 + f;
       if (a.out_f32) ((float*)a.out)[at] = y;
       else elem<bf16_t>::store((bf16_t*)a.out + at, y);
     }

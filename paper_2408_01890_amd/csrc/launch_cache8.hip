@@ -74,7 +74,7 @@ template int launch_cache8_concat<LISA_PART - 2>(const lisa_desc*, const Cache8S
 namespace {
 template <int FMT, int DK, int MODE, int GT, int GH>
 int launch_pv_nw(const lisa_desc* d, int wide, const Cache8PvArgs& a, hipStream_t st) {
-  const dim3 grid(d->Hkv * a.chunks, a.n_span, d->B);
+  const dim3 grid(d->Hkv * a.chunks * a.f_parts, a.n_span, d->B);
   StageScope prof("k_cache8_pv", st);
   constexpr bool EIGHT = MODE > 0 && GT == 1;                // (pv_geom)
   if (EIGHT && wide) k_cache8_pv<FMT, DK, MODE, GT, GH, EIGHT ? 8 : 4><<<grid, 512, 0, st>>>(a);
@@ -97,7 +97,7 @@ int launch_pv_mode(const lisa_desc* d, int mode, int wide, const Cache8PvArgs& a
 }  // namespace
 template <int FMT>
 int launch_cache8_pv(const lisa_desc* d, int mode, int wide, const Cache8PvArgs& a, hipStream_t st) {
-  return d->d_k == 128 ? launch_pv_mode<FMT, 128>(d, mode, wide, a, st) : launch_pv_mode<FMT, 64>(d, mode, wide, a, st);
+  return d->d_k / a.f_parts == 128 ? launch_pv_mode<FMT, 128>(d, mode, wide, a, st) : launch_pv_mode<FMT, 64>(d, mode, wide, a, st);
 }
 template int launch_cache8_pv<LISA_PART - 4>(const lisa_desc*, int, int, const Cache8PvArgs&, hipStream_t);
 #else
@@ -124,14 +124,18 @@ Module module_of(const lisa_desc* d) {
 // Four for standard layers (fewer leave their registers room; 32 sequences of up to 8192, 8 kv heads: 76 us, 85 at eight spans instead of one),
 // where a wave has more than four heads (256 registers do not hold them with eight) and where several workgroups per compute unit with 32
 // pages at most follow one another (64 sequences of up to 500 tokens, 32 heads: 35 us, with eight 43; at 2500 129 and 126).
+// Features are dealt to two workgroups, which needs no merging, where that spares a split or none is made anyway (LiSA, 16 sequences of up to 1000
+// tokens, 8 kv heads: 14.6 us, 15.7 without; with splits it only adds workgroups: 4 of 3000 17.4 and 17.0).
 struct PvGeom {
-  int wide, span_pages, n_span, chunks;
+  int wide, span_pages, n_span, chunks, f_parts;
 };
 PvGeom pv_geom(const lisa_desc* d, bool lisa_layer) {
   const int group = d->H / d->Hkv, n_pages = std::max((d->Lk + PG_TOK - 1) / PG_TOK, 1);
   PvGeom g;
   g.chunks = group <= 4 ? 1 : (group + 7) / 8;
-  const long long base = (long long)d->B * d->Hkv * g.chunks;
+  long long base = (long long)d->B * d->Hkv * g.chunks;
+  g.f_parts = lisa_layer && d->d_k == 128 && base <= 128 && (n_pages <= 16 || base == 128) ? 2 : 1;
+  base *= g.f_parts;
   g.wide = lisa_layer && group <= 4 && (base < 512 || n_pages > 32);
   const int waves = g.wide ? 8 : 4;
   const int spans = n_pages <= 16 ? 1 : (int)std::min<long long>((256 + base - 1) / base, (n_pages + 7) / 8);
@@ -222,6 +226,7 @@ int run_cache8_fast(const lisa_desc* d, bool lisa_layer, int fmt, const Cache8Vi
   p.n_span = g.n_span;
   p.span_pages = g.span_pages;
   p.chunks = g.chunks;
+  p.f_parts = g.f_parts;
   p.out_f32 = d->out_f32;
   p.scale = scale;
   const int mode = !lisa_layer ? 0 : share ? 2 : 1;
