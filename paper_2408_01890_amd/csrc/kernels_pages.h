@@ -47,24 +47,57 @@ __device__ __forceinline__ int pgs_scan(int v, int& total, PgsScan& s) {
   return before + v;
 }
 
-// ids[0 .. n) = the first pages for which pick(page) holds, from page `from` on, n <= want of them; returns n.  (Every thread calls it.)
-template <class Pick>
-__device__ __forceinline__ int pgs_collect(const PagesView& g, int from, int to, int want, int* ids, PgsScan& s, Pick&& pick) {
-  int found = 0;
-  for (int p0 = from; p0 < to && found < want; p0 += 4 * PGS_THREADS) {
-    const int p = p0 + 4 * (int)threadIdx.x;
-    bool in[4];
-    int n = 0;
+// The counts of eight pages per thread, of 8192 in all.  A kernel asks for the first 8192 (`first`) when it begins, beside what else it reads: what it
+// spends is a chain of reads and barriers of about a microsecond each.
+constexpr int PGS_EACH = 8;
+struct PgsRefs {
+  int r[PGS_EACH];
+  __device__ __forceinline__ void load(const PagesView& g, int p0) {
+    typedef int i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+    const int p = p0 + PGS_EACH * (int)threadIdx.x;
+    if (p + PGS_EACH <= g.P) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      in[u] = p + u < to && pick(g.refs[min(p + u, g.P - 1)]);
-      n += in[u];
+      for (int q = 0; q < PGS_EACH / 4; ++q) {
+        const i32x4_a4 x = *(const i32x4_a4*)(g.refs + p + 4 * q);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) r[4 * q + u] = x[u];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < PGS_EACH; ++u) r[u] = g.refs[min(p + u, g.P - 1)];
     }
+  }
+};
+// A list of pages, the first 2048 of them in the LDS.
+constexpr int PGS_LDS_IDS = 2048;
+struct PgsList {
+  int* lds;
+  int* rest;               // [P] of the workspace
+  __device__ __forceinline__ void put(int i, int p) const {
+    if (i < PGS_LDS_IDS) lds[i] = p;
+    else rest[i] = p;
+  }
+  __device__ __forceinline__ int get(int i) const { return i < PGS_LDS_IDS ? lds[i] : rest[i]; }
+};
+// list[0 .. n) = the first pages in [from, to) for which pick(refs) holds, n <= want of them; returns n.  (Every thread calls it.)
+template <class Pick>
+__device__ __forceinline__ int pgs_collect(const PagesView& g, const PgsRefs& first, int from, int to, int want, const PgsList& list, PgsScan& s,
+                                           Pick&& pick) {
+  constexpr int CHUNK = PGS_EACH * PGS_THREADS;
+  int found = 0;
+  for (int p0 = from / CHUNK * CHUNK; p0 < to && found < want; p0 += CHUNK) {
+    PgsRefs x = first;
+    if (p0) x.load(g, p0);
+    const int p = p0 + PGS_EACH * (int)threadIdx.x;
+    unsigned in = 0;
+#pragma unroll
+    for (int u = 0; u < PGS_EACH; ++u) in |= (p + u >= from && p + u < to && pick(x.r[u]) ? 1u : 0u) << u;
+    const int n = __popc(in);
     int total, at = found + pgs_scan(n, total, s) - n;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (in[u]) {
-        if (at < want) ids[at] = p + u;
+    for (int u = 0; u < PGS_EACH; ++u)
+      if (in >> u & 1) {
+        if (at < want) list.put(at, p + u);
         ++at;
       }
     found += total;
@@ -73,60 +106,66 @@ __device__ __forceinline__ int pgs_collect(const PagesView& g, int from, int to,
   return min(found, want);
 }
 
-// owner[s] = the first request that names s among those that `good` accepts.
-template <class Good>
-__device__ __forceinline__ void pgs_owners(const PagesView& g, const int* named, int n, Good&& good) {
-  for (int s = threadIdx.x; s < g.S; s += PGS_THREADS) g.owner[s] = n;
+// owner(s) = the first request that names s, in the LDS where 2048 sequences are all.
+constexpr int PGS_LDS_OWNERS = 2048;
+__device__ __forceinline__ int* pgs_owners_clear(const PagesView& g, int* lds, int n) {
+  int* owner = g.S <= PGS_LDS_OWNERS ? lds : g.owner;
+  for (int s = threadIdx.x; s < g.S; s += PGS_THREADS) owner[s] = n;
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += PGS_THREADS)
-    if (good(i)) atomicMin(g.owner + named[i], i);
-  __syncthreads();
+  return owner;
 }
 
 // Sequence s is given add[s] more tokens and the pages they need.
 __global__ __launch_bounds__(PGS_THREADS) void k_pages_grow(PagesView g, const int* __restrict__ add, int* __restrict__ done) {
   __shared__ PgsScan scan;
-  __shared__ int base_s[PGS_THREADS], more_s[PGS_THREADS];
+  __shared__ int base_s[PGS_THREADS], more_s[PGS_THREADS], have_s[PGS_THREADS], ids_s[PGS_LDS_IDS];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  auto fits = [&](int s, int& more) {
-    const long long want = (long long)g.lens[s] + add[s];
-    const bool ok = add[s] >= 0 && g.lens[s] >= 0 && want <= (long long)g.C * 64;
-    more = ok ? pages_of((int)want) - pages_of(g.lens[s]) : 0;
+  PgsRefs first;
+  first.load(g, 0);
+  int len, inc, more;                                        // of sequence s0 + tid: its tokens, those added, the pages they need
+  auto read = [&](int s0) {
+    const int s = min(s0 + tid, g.S - 1);
+    len = g.lens[s], inc = add[s];
+    const long long want = (long long)len + inc;
+    const bool ok = s0 + tid < g.S && inc >= 0 && len >= 0 && want <= (long long)g.C * 64;
+    more = ok ? pages_of((int)want) - pages_of(len) : 0;
     return ok;
   };
+  const bool one = g.S <= PGS_THREADS;                       // (all sequences at once: they are read once)
   int want = 0;                                              // pages wanted by all (no more than there are)
+  bool ok = false;
   for (int s0 = 0; s0 < g.S; s0 += PGS_THREADS) {
-    int more = 0, total;
-    if (s0 + tid < g.S) fits(s0 + tid, more);
+    int total;
+    ok = read(s0);
     (void)pgs_scan(min(more, g.P), total, scan);
     want = (int)min((long long)want + total, (long long)g.P);
   }
-  const int found = pgs_collect(g, 0, g.P, want, g.ids, scan, [](int r) { return r == 0; });
+  const PgsList ids{ids_s, g.ids};
+  const int found = pgs_collect(g, first, 0, g.P, want, ids, scan, [](int r) { return r == 0; });
   long long given = 0;
   for (int s0 = 0; s0 < g.S; s0 += PGS_THREADS) {
     const int s = s0 + tid;
-    int more = 0, total;
-    const bool ok = s < g.S && fits(s, more);
-    const int capped = min(more, g.P + 1);                   // (no sum of 1024 of them passes 32 bits: P is below 2^20)
+    if (!one) ok = read(s0);
+    int total;
+    const int capped = min(more, g.P + 1);                   // (no sum of 1024 of them passes 32 bits: P is at most 2^20)
     const long long upto = given + pgs_scan(capped, total, scan);
     const bool yes = ok && (more == 0 || upto <= found);
     base_s[tid] = (int)(upto - capped);
     more_s[tid] = yes ? more : 0;
+    have_s[tid] = pages_of(max(len, 0));
     given += total;
     __syncthreads();
     for (int u = wv; u < PGS_THREADS && s0 + u < g.S; u += PGS_THREADS / 64) {
       const int m = more_s[u];
-      if (!m) continue;
-      const int have = pages_of(g.lens[s0 + u]);
       for (int c = lane; c < m; c += 64) {
-        const int p = g.ids[base_s[u] + c];
-        g.table[(size_t)(s0 + u) * g.C + have + c] = p;
+        const int p = ids.get(base_s[u] + c);
+        g.table[(size_t)(s0 + u) * g.C + have_s[u] + c] = p;
         g.refs[p] = 1;
       }
     }
-    __syncthreads();                                         // (lens are read above)
+    __syncthreads();                                         // (the next 1024 use the same LDS)
     if (s < g.S) {
-      if (yes) g.lens[s] += add[s];
+      if (yes) g.lens[s] = len + inc;
       done[s] = yes;
     }
   }
@@ -134,11 +173,15 @@ __global__ __launch_bounds__(PGS_THREADS) void k_pages_grow(PagesView g, const i
 
 // The sequences named give their pages back.
 __global__ __launch_bounds__(PGS_THREADS) void k_pages_free(PagesView g, const int* __restrict__ seqs, int n, int* __restrict__ done) {
+  __shared__ int owner_s[PGS_LDS_OWNERS];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  pgs_owners(g, seqs, n, [&](int i) { return (unsigned)seqs[i] < (unsigned)g.S; });
+  int* owner = pgs_owners_clear(g, owner_s, n);
+  for (int i = threadIdx.x; i < n; i += PGS_THREADS)
+    if ((unsigned)seqs[i] < (unsigned)g.S) atomicMin(owner + seqs[i], i);
+  __syncthreads();
   for (int i = wv; i < n; i += PGS_THREADS / 64) {
     const int s = seqs[i];
-    const bool yes = (unsigned)s < (unsigned)g.S && g.owner[s] == i;
+    const bool yes = (unsigned)s < (unsigned)g.S && owner[s] == i;
     if (yes) {
       const int have = min(pages_of(max(g.lens[s], 0)), g.C);
       for (int c = lane; c < g.C; c += 64) {
@@ -157,45 +200,58 @@ __global__ __launch_bounds__(PGS_THREADS) void k_pages_free(PagesView g, const i
 __global__ __launch_bounds__(PGS_THREADS) void k_pages_fork(PagesView g, const int* __restrict__ src, const int* __restrict__ dst, int n,
                                                             int* __restrict__ done, int2* __restrict__ copies) {
   __shared__ PgsScan scan;
-  __shared__ int base_s[PGS_THREADS];
+  __shared__ int to_s[PGS_THREADS], src_s[PGS_THREADS], dst_s[PGS_THREADS], len_s[PGS_THREADS], ids_s[PGS_LDS_IDS], owner_s[PGS_LDS_OWNERS];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  auto good = [&](int i) {
-    return (unsigned)src[i] < (unsigned)g.S && (unsigned)dst[i] < (unsigned)g.S && src[i] != dst[i] && g.lens[dst[i]] == 0;
+  PgsRefs first;
+  first.load(g, 0);
+  int from, into, len;                                       // of request i0 + tid: its sequences, the length of the one (-1: not this request)
+  auto read = [&](int i) {
+    from = src[min(i, n - 1)], into = dst[min(i, n - 1)];
+    const bool named = i < n && (unsigned)from < (unsigned)g.S && (unsigned)into < (unsigned)g.S && from != into;
+    const int there = g.lens[named ? into : 0], tokens = g.lens[named ? from : 0];
+    len = named && there == 0 ? min(max(tokens, 0), g.C * 64) : -1;
   };
-  pgs_owners(g, dst, n, good);
+  const bool one = n <= PGS_THREADS;                         // (all requests at once: they are read once)
+  read(tid);
+  int* owner = pgs_owners_clear(g, owner_s, n);
+  for (int i = tid; i < n; i += PGS_THREADS) {
+    if (!one) read(i);
+    if (len >= 0) atomicMin(owner + into, i);
+  }
+  __syncthreads();
   int want = 0;
-  for (int i0 = 0; i0 < n; i0 += PGS_THREADS) {              // lengths before the call (-1: not this one)
+  for (int i0 = 0; i0 < n; i0 += PGS_THREADS) {
     const int i = i0 + tid;
-    int part = 0, total;
-    if (i < n) {
-      const bool yes = good(i) && g.owner[dst[i]] == i;
-      const int len = yes ? min(max(g.lens[src[i]], 0), g.C * 64) : -1;
-      g.info[i] = len;
-      part = yes && len % 64 != 0;
-    }
+    int total;
+    if (!one) read(i);
+    if (len >= 0 && owner[into] != i) len = -1;
+    if (!one && i < n) g.info[i] = len;                      // (before the call: what is given below changes lens)
+    const int part = len >= 0 && len % 64 != 0;
     (void)pgs_scan(part, total, scan);
     want += total;
   }
-  const int found = pgs_collect(g, 0, g.P, min(want, g.P), g.ids, scan, [](int r) { return r == 0; });
+  const PgsList ids{ids_s, g.ids};
+  const int found = pgs_collect(g, first, 0, g.P, min(want, g.P), ids, scan, [](int r) { return r == 0; });
   int given = 0;
   for (int i0 = 0; i0 < n; i0 += PGS_THREADS) {
     const int i = i0 + tid;
-    const int len = i < n ? g.info[i] : -1;
+    if (!one) from = src[min(i, n - 1)], into = dst[min(i, n - 1)], len = i < n ? g.info[i] : -1;
     const int part = len >= 0 && len % 64 != 0;
     int total;
     const int upto = given + pgs_scan(part, total, scan);
     const bool yes = len >= 0 && (!part || upto <= found);
     given += total;
-    base_s[tid] = yes ? (part ? g.ids[upto - 1] : -2) : -1;  // the copy's page, -2: none needed, -1: not this one
+    const int to = yes ? (part ? ids.get(upto - 1) : -2) : -1;   // the copy's page, -2: none needed, -1: not this one
+    to_s[tid] = to, len_s[tid] = len, src_s[tid] = from, dst_s[tid] = into;
     if (i < n) {
       done[i] = yes;
-      copies[i] = yes && part ? make_int2(g.table[(size_t)src[i] * g.C + len / 64], base_s[tid]) : make_int2(-1, -1);
+      copies[i] = yes && part ? make_int2(g.table[(size_t)from * g.C + len / 64], to) : make_int2(-1, -1);
     }
     __syncthreads();
     for (int u = wv; u < PGS_THREADS && i0 + u < n; u += PGS_THREADS / 64) {
-      const int to = base_s[u];
+      const int to = to_s[u];
       if (to == -1) continue;
-      const int a = src[i0 + u], d = dst[i0 + u], full = g.info[i0 + u] / 64;
+      const int a = src_s[u], d = dst_s[u], full = len_s[u] / 64;
       for (int c = lane; c < g.C; c += 64) {
         int p = -1;
         if (c < full) {
@@ -207,7 +263,7 @@ __global__ __launch_bounds__(PGS_THREADS) void k_pages_fork(PagesView g, const i
         }
         g.table[(size_t)d * g.C + c] = p;
       }
-      if (lane == 0) g.lens[d] = g.info[i0 + u];
+      if (lane == 0) g.lens[d] = len_s[u];
     }
     __syncthreads();
   }
@@ -217,20 +273,25 @@ __global__ __launch_bounds__(PGS_THREADS) void k_pages_fork(PagesView g, const i
 // page p goes (or p), copies[i] = (from, to), then (-1, -1).
 __global__ __launch_bounds__(PGS_THREADS) void k_pages_compact(PagesView g, int2* __restrict__ copies, int n_copies) {
   __shared__ PgsScan scan;
+  __shared__ int to_s[PGS_LDS_IDS], from_s[PGS_LDS_IDS];
   const int tid = threadIdx.x;
+  PgsRefs first;
+  first.load(g, 0);
   int used = 0;
-  for (int p0 = 0; p0 < g.P; p0 += 4 * PGS_THREADS) {
+  for (int p0 = 0; p0 < g.P; p0 += PGS_EACH * PGS_THREADS) {
+    PgsRefs x = first;
+    if (p0) x.load(g, p0);
     int n = 0, total;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) n += p0 + 4 * tid + u < g.P && g.refs[min(p0 + 4 * tid + u, g.P - 1)] > 0;
+    for (int u = 0; u < PGS_EACH; ++u) n += p0 + PGS_EACH * tid + u < g.P && x.r[u] > 0;
     (void)pgs_scan(n, total, scan);
     used += total;
   }
   // holes in front, used pages behind
-  int* from = g.ids + g.P;
-  const int moves = pgs_collect(g, 0, used, n_copies, g.ids, scan, [](int r) { return r <= 0; });
-  (void)pgs_collect(g, used, g.P, n_copies, from, scan, [](int r) { return r > 0; });
-  for (int i = tid; i < n_copies; i += PGS_THREADS) copies[i] = i < moves ? make_int2(from[i], g.ids[i]) : make_int2(-1, -1);
+  const PgsList to{to_s, g.ids}, from{from_s, g.ids + g.P};
+  const int moves = pgs_collect(g, first, 0, used, n_copies, to, scan, [](int r) { return r <= 0; });
+  (void)pgs_collect(g, first, used, g.P, n_copies, from, scan, [](int r) { return r > 0; });
+  for (int i = tid; i < n_copies; i += PGS_THREADS) copies[i] = i < moves ? make_int2(from.get(i), to.get(i)) : make_int2(-1, -1);
   __syncthreads();
   for (int p = tid; p < g.P; p += PGS_THREADS) g.ids[p] = p;
   __syncthreads();

@@ -21,7 +21,7 @@ def equal(pages, ref):
     assert pages.refs.tolist() == ref.refs
 
 
-@pytest.mark.parametrize("P,S,C,seed", [(1, 1, 1, 0), (7, 3, 2, 1), (40, 9, 6, 2), (300, 33, 20, 3), (5000, 70, 100, 4), (9000, 1500, 9, 5), (64, 2000, 3, 6)])
+@pytest.mark.parametrize("P,S,C,seed", [(1, 1, 1, 0), (7, 3, 2, 1), (40, 9, 6, 2), (300, 33, 20, 3), (5000, 70, 100, 4), (9000, 1500, 9, 5), (64, 2000, 3, 6), (3000, 2600, 3, 7)])
 def test_random_calls_equal_the_lists(P, S, C, seed):
     r = random.Random(seed)
     pages, ref = lisa.Pages.empty(P, S, C, DEV), cr.RefPages(P, S, C)
