@@ -312,6 +312,59 @@ struct FfnStage {
   }
 };
 
+// The FFN of sixteen tokens from the image of MfmaFfn::stage().  What is not a half number already, A_delta and the hidden units, goes in as two (x and what
+// is left of it, 2^-22 together): rounded to one half each, these add as much to a row's error as the half number that it is handed on in.
+// 32 hidden units at a time; the weights of the next 32 are read while these are multiplied.
+template <int ACT, int KX, int FS, int HBO, bool LO>
+__device__ __forceinline__ void cache8_ffn(const unsigned short* lds, const f16x8 (&x)[KX], const f16x8 (&xl)[LO ? KX : 1], f32x4 (&y)[HBO]) {
+  const int lane = threadIdx.x & 63;
+  const unsigned short* l1 = lds + lane * 8;
+  const unsigned short* l2 = l1 + 2 * FS * KX * 512;
+  f16x8 w1[2][2][KX], w2[2][HBO];
+  auto read = [&](int s, f16x8 (&a)[2][KX], f16x8 (&b)[HBO]) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int ks = 0; ks < KX; ++ks) a[half][ks] = *(const f16x8*)(l1 + ((2 * s + half) * KX + ks) * 512);
+#pragma unroll
+    for (int hb = 0; hb < HBO; ++hb) b[hb] = *(const f16x8*)(l2 + (hb * FS + s) * 512);
+  };
+  read(0, w1[0], w2[0]);
+#pragma unroll
+  for (int hb = 0; hb < HBO; ++hb) y[hb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < FS; ++s) {
+    if (s + 1 < FS) read(s + 1, w1[(s + 1) & 1], w2[(s + 1) & 1]);
+    f16x8 hi, lo;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KX; ++ks) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w1[s & 1][half][ks], x[ks], acc, 0, 0, 0);
+        if (LO) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w1[s & 1][half][ks], xl[LO ? ks : 0], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        float u = acc[v];
+        if (ACT == 1) {                                      // (exp2 of a very negative u: inf, 1 / inf = 0)
+          u = fminf(u * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u)), 65504.f);
+        } else {
+          u = __builtin_amdgcn_fmed3f(u, 0.f, 65504.f);
+        }
+        hi[4 * half + v] = (half_t)u;
+        lo[4 * half + v] = (half_t)(u - (float)hi[4 * half + v]);
+      }
+    }
+#pragma unroll
+    for (int hb = 0; hb < HBO; ++hb) {
+      y[hb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w2[s & 1][hb], hi, y[hb], 0, 0, 0);
+      y[hb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w2[s & 1][hb], lo, y[hb], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // MODE 0: A_n = A_{n-1} + A_delta, 1: FFN(A_{n-1}) + A_delta, 2: FFN([A_{n-1}; A_delta]).  KS: pieces of 32 features of a K_LR row.
 // grid (ceil(pages / n_pages), B), block 256: n_pages pages of a sequence, all heads.  Per page the waves take tiles of four heads in turn
 // (A_delta to the LDS), then 16 tokens each through the FFN; the next page's keys and A_{n-1} are loaded where this one's have been used, and one
@@ -472,21 +525,29 @@ __global__ __launch_bounds__(256, 2) void k_cache8_scores_mfma(Cache8ScoresArgs 
     } else {
       // (what follows from the lane's number is made anew: kept over the pages, it does not fit the registers)
       int go = g, po = pj;
-      if (MODE == 2) asm volatile("" : "+v"(go), "+v"(po));
-      f16x8 x[1][KX];
+      asm volatile("" : "+v"(go), "+v"(po));
+      f16x8 x[KX], xl[MODE == 2 ? KX : 1];
 #pragma unroll
       for (int ks = 0; ks < KX; ++ks)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int ch = 32 * ks + 8 * go + e;
-          x[0][ks][e] = ks < KP ? __builtin_bit_cast(half_t, xin[ks < KP ? ks : 0][e]) : (_Float16)0.f;
-          if (MODE == 2 && ch >= H) x[0][ks][e] = ch < Din ? f32_to_half_sat(to[(ch - H) * C8_SROW + po]) : (_Float16)0.f;
-          else if (ch >= Din) x[0][ks][e] = (_Float16)0.f;
+          x[ks][e] = ks < KP ? __builtin_bit_cast(half_t, xin[ks < KP ? ks : 0][e]) : (_Float16)0.f;
+          if constexpr (MODE == 2) {
+            float u = 0.f;
+            if (ch >= H) {
+              u = ch < Din ? to[(ch - H) * C8_SROW + po] : 0.f;
+              x[ks][e] = f32_to_half_sat(u);
+              u -= (float)x[ks][e];
+            }
+            xl[ks][e] = f32_to_half_sat(u);
+          } else if (ch >= Din) {
+            x[ks][e] = (_Float16)0.f;
+          }
         }
       if (MORE) load_x(next);
-      f32x4 y[1][HBO];
-      if (MODE == 2) Ffn::template apply_lds_lean<1>(w_s, x, y);
-      else Ffn::template apply_lds<1>(w_s, x, y);
+      f32x4 y[HBO];
+      cache8_ffn<ACT, KX, FS, HBO, MODE == 2>(w_s, x, xl, y);
       // this wave's tokens of the tile become A_n (no other wave has business with them), and go out as rows
       float d[HBO][4];
 #pragma unroll
@@ -497,7 +558,7 @@ __global__ __launch_bounds__(256, 2) void k_cache8_scores_mfma(Cache8ScoresArgs 
       for (int hb = 0; hb < HBO; ++hb)
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          to[min(16 * hb + 4 * go + v, H) * C8_SROW + po] = y[0][hb][v] + d[hb][v];
+          to[min(16 * hb + 4 * go + v, H) * C8_SROW + po] = y[hb][v] + d[hb][v];
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int hb = 0; hb < HBO; ++hb)
