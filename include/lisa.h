@@ -439,7 +439,8 @@ int lisa_cache8_append(const lisa_desc* desc, const lisa_cache8* cache, const vo
  * 8-bit cache that holds the new token already.  desc: dtype, B, H, Hkv, d_k, r, F, mix, act, scales, write_scores, out_f32 as there,
  * Lq = 1, Lk = width of the score rows and an upper bound of the lengths (<= max_pages * 64); causal, Lmax and kcache_dim_major are not
  * used.  Sequence b attends its first min(lens[b], Lk) tokens; the score rows' entries past them are neither read nor written, a
- * sequence without tokens gives zeros.
+ * sequence without tokens gives zeros.  NaN among a token's keys (possible in e4m3 codes only) makes NaN of its A_delta for the heads
+ * that read them and, in a LiSA layer, for up to three neighbouring heads, whose products share an accumulator.
  *   q_lr [B,H,r] / q [B,H,d_k]   in   (q_lr NULL: LISA_MIX_SHARE)
  *   score_row_prev [B,H,Lk]      in   A_{n-1}, score type
  *   w1, w2                       in   as in lisa_attn_decode
@@ -459,7 +460,7 @@ int std_attn_decode8(const lisa_desc* desc, const lisa_cache8* cache, const void
  * requests are served in the order of their index, free pages are given in ascending order.
  */
 typedef struct lisa_pages {
-  int32_t n_pages;          /* pages of every pool, below 2^20                                 */
+  int32_t n_pages;          /* pages of every pool, at most 2^20                               */
   int32_t n_seqs;           /* rows of the table                                               */
   int32_t max_pages;        /* columns of the table                                            */
   int32_t reserved;         /* 0                                                               */

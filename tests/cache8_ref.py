@@ -87,10 +87,12 @@ class RefCache:
 def decode(ref, table, lens, Lk, q, prev, w1, w2, mix, act, scale, dk, H):
     """A decode step in float64.  mix: 'add', 'concat', 'plus', 'share', 'std'.  Returns per sequence (rows [H, n], out [H, dk],
     there [n], row_bound [H, n], out_bound [H, dk]): how far a kernel may be off that keeps to what the library says of
-    its precision - A_{n-1}, hidden units, A_delta as an FFN input and emitted scores in half (2^-11 of each), sums in
-    float32 (2^-24 a term), probabilities to 2^-11.  float32 calls have no half and keep probabilities to 2^-22."""
+    its precision - A_{n-1} and emitted scores in half (2^-11 of each), hidden units and A_delta as an FFN input as two half numbers (2^-22 of
+    each; a second one below 2^-14 is a whole number of 2^-24), sums in float32 (2^-24 a term), probabilities to 2^-11.  float32 calls have no
+    half and keep probabilities to 2^-22."""
     f32 = q is not None and q.dtype == torch.float32 or prev is not None and prev.dtype == torch.float32
     half = 2.0 ** -24 if f32 else 2.0 ** -11
+    two, least = (2.0 ** -24, 0.0) if f32 else (2.0 ** -22, 2.0 ** -25)
     out = []
     for b in range(len(lens)):
         n = max(0, min(int(lens[b]), Lk))
@@ -111,14 +113,14 @@ def decode(ref, table, lens, Lk, q, prev, w1, w2, mix, act, scale, dk, H):
             x = values(prev[b, :, :n])
             if mix in ("add", "concat"):
                 W1 = values(w1)
-                xin, ein = (np.concatenate([x, a]), np.concatenate([np.zeros_like(x), e + half * np.abs(a)])) if mix == "concat" else (x, np.zeros_like(x))
+                xin, ein = (np.concatenate([x, a]), np.concatenate([np.zeros_like(x), e + two * np.abs(a) + least])) if mix == "concat" else (x, np.zeros_like(x))
                 u = W1.T @ xin
                 eu = np.abs(W1).T @ ein + np.abs(W1).T @ np.abs(xin) * 2.0 ** -24 * (len(W1) + 4)
                 if act == "single":
-                    y, ey = u, eu + half * np.abs(u)
+                    y, ey = u, eu + two * np.abs(u) + least
                 else:
                     hid = np.maximum(u, 0) if act == "relu" else u / (1 + np.exp(-u))
-                    ehid = 1.1 * eu + (half + 2.0 ** -21) * np.abs(hid)
+                    ehid = 1.1 * eu + (two + 2.0 ** -21) * np.abs(hid) + least
                     W2 = values(w2)
                     y = W2.T @ hid
                     ey = np.abs(W2).T @ ehid + np.abs(W2).T @ np.abs(hid) * 2.0 ** -24 * (len(W2) + 4)
