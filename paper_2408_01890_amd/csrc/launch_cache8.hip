@@ -170,7 +170,7 @@ Ws ws_of(const lisa_desc* d, bool lisa_layer) {
 
 bool cache8_fast_ok(const lisa_desc* d, bool lisa_layer) {
   if (d->dtype != LISA_BF16 || (d->d_k != 64 && d->d_k != 128)) return false;
-  if ((long long)(d->H / d->Hkv + 7) / 8 * d->Hkv > 65535) return false;
+  if ((long long)(d->H / d->Hkv + 7) / 8 * d->Hkv > 65535 || d->Lk > 1 << 29) return false;   // (the grid: spans of 256 pages at the most)
   if (!lisa_layer || d->mix == LISA_MIX_SHARE) return true;
   if (d->r > 64 || d->H > 64 || (long long)d->H * d->Lk >= 1LL << 30) return false;   // (32-bit offsets in a sequence's score rows)
   if (d->mix == LISA_MIX_PLUS) return true;

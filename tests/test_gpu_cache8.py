@@ -271,6 +271,20 @@ def test_decode8_of_long_and_many_sequences(lens, mix, fmt):
         check_decode(g, FMT[fmt], torch.bfloat16, H, Hkv, 128, 128 if mix == "std" else 22, 16, mix, "relu", lens, write=False)
 
 
+@pytest.mark.parametrize("mix", ["add", "share", "std"])
+@pytest.mark.parametrize("H,Hkv,dk,lens,absent", [
+    (2, 1, 64, [36000], ()),                                 # more spans than a wave has lanes
+    (4, 1, 128, [1500, 40], [(0, c) for c in range(8)]),     # a span without a page, spans behind a sequence's end
+    (16, 2, 128, [150, 1], ()),                              # eight heads per kv head, features dealt to two workgroups
+    (8, 8, 128, [1100] * 16, ()),                            # features dealt to two workgroups of all pages
+    (8, 8, 64, [90] * 70, ()),                               # many short sequences: four waves
+    (8, 8, 64, [2100] * 64, ()),                             # many of more than 32 pages: eight
+])
+def test_decode8_however_the_work_is_dealt(H, Hkv, dk, lens, absent, mix):
+    g = torch.Generator().manual_seed(dk + len(lens))
+    check_decode(g, I8, torch.bfloat16, H, Hkv, dk, dk if mix == "std" else 22, 16, mix, "relu", lens, absent=absent)
+
+
 @pytest.mark.parametrize("mix", ["add", "concat", "share", "std"])
 @pytest.mark.parametrize("shape", [(32, 8, 128, 22, 64), (6, 2, 40, 9, 20)])
 def test_decode8_over_missing_pages_and_with_nan_behind_the_ends(shape, mix):
